@@ -16,6 +16,9 @@
  *   - tail-focused layer schedule (Eq. 3):  tf_tail_schedule, tf_filtered_attention_layers
  *   - one token at a time with caller-held state (Algorithm 1 as a call per token):
  *     tf_decode_init, tf_decode_prefill, tf_decode_step
+ *   - before it: norms of queries and keys and the position rotation:  tf_norm_rotate
+ *   - a cache in 4 or 8 bits:  tf_cache_bytes, tf_cache_write, tf_cache_read, tf_cache_attend; the
+ *     per-token form on such a cache:  tf_decode_prefill_q, tf_decode_step_q
  *   - measurement:  tf_stage_timing_*, tf_probe_*
  * Variants selected through tf_params: the incremental anchor of Eq. 1 (anchor, ema_gamma), the
  * anchor that includes the current token (anchor_inclusive), key-only / value-only scores and
@@ -292,6 +295,101 @@ tf_status tf_decode_prefill(tf_ctx *ctx, const tf_params *p, float eta, float ta
 tf_status tf_decode_step(tf_ctx *ctx, const tf_params *p, float eta, const tf_decode_state *state,
                          const void *q, const void *k, const void *v, void *o, uint8_t *skip,
                          float *fused, void *ws, size_t ws_bytes, void *stream);
+
+/* Norms of queries and keys for each head, and their rotation by position, in one pass (what comes
+ * between the projections and tf_score / tf_filtered_attention / tf_decode_step, which take Q and K as
+ * they are).  Per row x of 128 columns:
+ *   norm      y = x * w / sqrt(mean(x^2) + eps)          (w NULL: y = x)
+ *   rotation  angle = position * freq[j]; columns (j, j + rot_dim/2), or (2j, 2j + 1) if interleaved,
+ *             (a, b) -> (a cos - b sin, b cos + a sin); columns from rot_dim on are passed on.
+ * The position of token t of row b is (positions ? positions[b][t] : t) + (start ? start[b] : 0): with
+ * start = tf_decode_state.seen a new token turns by the number of tokens before it, skipped ones
+ * included.  Position times frequency is formed and reduced to less than a turn in double, everything
+ * else is fp32 with one rounding at the end, whatever the dtype. */
+typedef struct {
+    const float *q_weight, *k_weight; /* DEVICE [128] each; NULL: that tensor is not normalised */
+    const double *freq;               /* DEVICE [rot_dim / 2], radians per position (NULL if rot_dim is 0) */
+    const int32_t *positions;         /* DEVICE [batch][seq], or NULL */
+    const int32_t *start;             /* DEVICE [batch], or NULL */
+    float eps;                        /* > 0 */
+    int32_t rot_dim;                  /* columns that are rotated: a multiple of 16, 0 .. 128 */
+    int32_t interleaved;              /* 0 or 1 */
+    int32_t reserved;                 /* must be 0 */
+} tf_rotary;
+
+/* Q: p->q_stride, Q_out: p->o_stride, K and K_out: p->kv_stride.  An output may be its input (Q_out ==
+ * Q needs equal strides), otherwise they must not overlap.  Q and Q_out, or K and K_out, may both be
+ * NULL: that tensor is left out. */
+tf_status tf_norm_rotate(tf_ctx *ctx, const tf_params *p, const tf_rotary *r, const void *Q,
+                         const void *K, void *Q_out, void *K_out, void *stream);
+
+/* A cache in 4 or 8 bits.  A row of 128 columns is held as four blocks of 32, each of them codes and one
+ * scale s = 2^(E - 127), E in a byte: s is the smallest power of two, at least 2^-126, with max|x| <= 6 s
+ * (TF_CACHE_FP4) or 448 s (TF_CACHE_FP8), and a code is x / s rounded to nearest, ties to even, as e2m1
+ * (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) or e4m3.  Magnitudes must be below 2^126.
+ * Rows lie in pages of 64 for each (batch row, KV head): [batch][n_kv_heads][ceil(capacity / 64)][page],
+ * a page being 64 rows of codes (C = 64 or 128 bytes a row) and then 256 scale bytes.  With r the row in
+ * its page, c its column, e = C / 16 the bytes of eight columns:
+ *   keys    codes of columns 8i .. 8i+7 at r C + i e, E of block j at 64 C + 16 j 4 + (r % 16) 4 + r / 16
+ *   values  codes of columns 8i .. 8i+7 at (r / 4) 4 C + 4 i e + (r % 4) e,
+ *           E of block j at 64 C + (r / 4 % 4) 64 + 16 j + (r / 16) 4 + r % 4
+ * (a byte of 4-bit codes: the even column in its low half).
+ * Rows behind `len` are never used, whatever lies there; pages must be there as a whole. */
+typedef enum { TF_CACHE_FP4 = 4, TF_CACHE_FP8 = 8 } tf_cache_format;
+
+typedef struct {
+    void *k, *v;       /* DEVICE, tf_cache_bytes() each, 16-byte aligned */
+    int32_t *len;      /* DEVICE [batch]: rows held */
+    int32_t *overflow; /* DEVICE [batch], or NULL: set to 1 where a row did not fit */
+    int32_t capacity;  /* rows per (batch, head), >= 1 */
+    int32_t format;    /* tf_cache_format */
+} tf_cache;
+
+/* Bytes of the keys (as many for the values) of a cache of `capacity` rows per (batch row, KV head); 0 if
+ * p, the format or the capacity is invalid. */
+size_t tf_cache_bytes(const tf_params *p, int32_t format, int32_t capacity);
+
+/* Appends rows of K and V (p->kv_stride) to every batch row's cache, quantised, and moves len on.
+ *   kept_idx  [batch][m] positions in [0, seq), as tf_select or tf_select_online leave them, or NULL: rows
+ *             0 .. m-1
+ *   count     [batch]: how many of the m are written (0 .. m), or NULL: all m.  1 <= m <= seq.
+ * Rows that do not fit are left out and marked in cache->overflow. */
+tf_status tf_cache_write(tf_ctx *ctx, const tf_params *p, const tf_cache *cache, const void *K,
+                         const void *V, const int32_t *kept_idx, int32_t m, const int32_t *count,
+                         void *stream);
+
+/* Reads rows start[b] .. start[b] + seq - 1 (start NULL: from 0; negative: 0) back into rows 0 .. of K and
+ * V (p->kv_stride), exactly what the codes stand for.  Rows that the cache does not hold are left as they
+ * were. */
+tf_status tf_cache_read(tf_ctx *ctx, const tf_params *p, const tf_cache *cache, const int32_t *start,
+                        void *K, void *V, void *stream);
+
+/* Causal softmax attention of seq new tokens per row, whose keys and values are the last rows of the
+ * cache, over the cache: query t of row b sees the first len[b] - count[b] + t + 1 rows (count NULL: seq).
+ * Queries from count[b] on (padding), and any that see no row, get a zero output row.
+ *   Q  in  p->q_stride, O  out  p->o_stride (must not overlap), count  DEVICE [batch], 0 .. seq, or NULL
+ * Arithmetic: what the codes stand for enters exactly; fp32 softmax and accumulation; queries as they
+ * are; weights to 2^-16 of themselves for TF_BF16 (the output is rounded to bf16), to fp32 for TF_F32.
+ * A row's results, rounding included, follow from its own queries, keys, len and count, `p` and
+ * cache->capacity alone. */
+tf_status tf_cache_attend(tf_ctx *ctx, const tf_params *p, const tf_cache *cache, const void *Q, void *O,
+                          const int32_t *count, void *ws, size_t ws_bytes, void *stream);
+
+/* Bytes of workspace for tf_cache_attend and tf_decode_step_q (0 if p is invalid). */
+size_t tf_cache_workspace_bytes(const tf_params *p);
+
+/* tf_decode_prefill and tf_decode_step on caches of `format`: state->k_cache and v_cache are then as
+ * described above, tf_cache_bytes(p, format, state->capacity) each, and a kept token is quantised as it is
+ * appended.  Scores, decisions, anchors and counters are the same as on caches of p->dtype (the filter never
+ * reads the cache); a decoded token attends over what the codes stand for, the token itself included, while
+ * the prompt's own tokens attend over K and V as given.  tf_decode_init serves both. */
+tf_status tf_decode_prefill_q(tf_ctx *ctx, const tf_params *p, float eta, float tau0,
+                              const tf_decode_state *state, int32_t format, const void *Q, const void *K,
+                              const void *V, uint8_t *keep, int32_t *kept_idx, int32_t *count,
+                              float *fused, void *O, void *ws, size_t ws_bytes, void *stream);
+tf_status tf_decode_step_q(tf_ctx *ctx, const tf_params *p, float eta, const tf_decode_state *state,
+                           int32_t format, const void *q, const void *k, const void *v, void *o,
+                           uint8_t *skip, float *fused, void *ws, size_t ws_bytes, void *stream);
 
 /* Tail-focused layer schedule (Section 3.3, Eq. 3), host side: to meet the global budget
  * p_global in [0, 1], the last ceil(tail_fraction * n_layers) layers (0 < tail_fraction <= 1)

@@ -20,6 +20,7 @@ TF_OK, TF_ERR_INVALID_ARG, TF_ERR_UNSUPPORTED, TF_ERR_WORKSPACE_TOO_SMALL, TF_ER
 TF_F32, TF_BF16 = 0, 1
 TF_FUSE_EQ2, TF_FUSE_INVVAR, TF_FUSE_KEY_ONLY, TF_FUSE_VALUE_ONLY = range(4)
 TF_ANCHOR_MEAN, TF_ANCHOR_EMA = 0, 1
+TF_CACHE_FP4, TF_CACHE_FP8 = 4, 8
 TF_N_STAGES = 6
 STAGE_NAMES = ("score", "fuse", "select", "compact", "zero_rows", "attend")
 
@@ -29,7 +30,9 @@ EXPORTS = ("tf_create", "tf_destroy", "tf_status_string", "tf_last_error", "tf_k
            "tf_probe_mfma_bf16", "tf_tail_schedule", "tf_filtered_attention_layers",
            "tf_select_online", "tf_attend_ragged", "tf_filtered_attention_online",
            "tf_decode_workspace_bytes", "tf_decode_init", "tf_decode_step", "tf_decode_prefill",
-           "tf_filtered_attention_static")
+           "tf_filtered_attention_static", "tf_norm_rotate", "tf_cache_bytes", "tf_cache_write",
+           "tf_cache_read", "tf_cache_attend", "tf_cache_workspace_bytes", "tf_decode_prefill_q",
+           "tf_decode_step_q")
 TF_STATIC_SCRATCH_BYTES = 16 << 20
 
 
@@ -50,6 +53,18 @@ class tf_decode_state(ctypes.Structure):
                 ("cache_len", ctypes.c_void_p), ("overflow", ctypes.c_void_p),
                 ("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p),
                 ("capacity", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class tf_rotary(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("freq", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("start", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class tf_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("len", ctypes.c_void_p),
+                ("overflow", ctypes.c_void_p), ("capacity", ctypes.c_int32), ("format", ctypes.c_int32)]
 
 
 class TokfiltError(RuntimeError):
@@ -112,6 +127,20 @@ def lib():
         L.tf_decode_step.restype = ctypes.c_int
         L.tf_decode_prefill.argtypes = [vp, pp, flt, flt, sp] + [vp] * 9 + [sz, vp]
         L.tf_decode_prefill.restype = ctypes.c_int
+        rp, cp = ctypes.POINTER(tf_rotary), ctypes.POINTER(tf_cache)
+        L.tf_norm_rotate.argtypes = [vp, pp, rp, vp, vp, vp, vp, vp]
+        L.tf_cache_bytes.argtypes = [pp, i32, i32]
+        L.tf_cache_bytes.restype = sz
+        L.tf_cache_workspace_bytes.argtypes = [pp]
+        L.tf_cache_workspace_bytes.restype = sz
+        L.tf_cache_write.argtypes = [vp, pp, cp, vp, vp, vp, i32, vp, vp]
+        L.tf_cache_read.argtypes = [vp, pp, cp, vp, vp, vp, vp]
+        L.tf_cache_attend.argtypes = [vp, pp, cp, vp, vp, vp, vp, sz, vp]
+        L.tf_decode_prefill_q.argtypes = [vp, pp, flt, flt, sp, i32] + [vp] * 9 + [sz, vp]
+        L.tf_decode_step_q.argtypes = [vp, pp, flt, sp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        for name in ("tf_norm_rotate", "tf_cache_write", "tf_cache_read", "tf_cache_attend",
+                     "tf_decode_prefill_q", "tf_decode_step_q"):
+            getattr(L, name).restype = ctypes.c_int
         L.tf_probe_hbm_read.argtypes = [vp, vp, sz, vp, vp, ctypes.POINTER(ctypes.c_double)]
         L.tf_probe_mfma_bf16.argtypes = [vp, i32, vp, vp, ctypes.POINTER(ctypes.c_double)]
         for name in ("tf_score", "tf_select", "tf_attend", "tf_filtered_attention",
@@ -162,6 +191,24 @@ def make_params(q_shape, kv_shape, dtype: torch.dtype, prune_ratio: float, warmu
     return p
 
 
+def make_rotary(freq: Optional[torch.Tensor], rot_dim: int, q_weight=None, k_weight=None,
+                positions=None, start=None, eps: float = 1e-6, interleaved: bool = False) -> tf_rotary:
+    """tf_rotary for tf_norm_rotate, from device tensors: freq float64 [rot_dim / 2] (radians per
+    position), q_weight / k_weight float32 [128] (None: no norm), positions int32 [batch, seq] and
+    start int32 [batch] (None: 0 .. seq - 1, and 0).  The tensors are kept alive with the result."""
+    for t, dt, what in ((freq, torch.float64, "freq"), (q_weight, torch.float32, "q_weight"),
+                        (k_weight, torch.float32, "k_weight"), (positions, torch.int32, "positions"),
+                        (start, torch.int32, "start")):
+        if t is not None and (t.dtype != dt or not t.is_contiguous()):
+            raise TokfiltError(TF_ERR_INVALID_ARG, "%s must be contiguous %s" % (what, dt))
+    r = tf_rotary()
+    r.freq, r.q_weight, r.k_weight = _ptr(freq), _ptr(q_weight), _ptr(k_weight)
+    r.positions, r.start = _ptr(positions), _ptr(start)
+    r.eps, r.rot_dim, r.interleaved = float(eps), int(rot_dim), int(bool(interleaved))
+    r.tensors = (freq, q_weight, k_weight, positions, start)
+    return r
+
+
 def tf_tail_schedule(n_layers: int, p_global: float, tail_fraction: float):
     """Per-layer pruning ratios of the tail-focused schedule; returns (ratios, n_tail)."""
     ratios = (ctypes.c_double * max(int(n_layers), 1))()
@@ -189,11 +236,36 @@ def tf_decode_workspace_bytes(p: tf_params) -> int:
     return int(lib().tf_decode_workspace_bytes(ctypes.byref(p)))
 
 
+def tf_cache_bytes(p: tf_params, format: int, capacity: int) -> int:
+    return int(lib().tf_cache_bytes(ctypes.byref(p), int(format), int(capacity)))
+
+
+def tf_cache_workspace_bytes(p: tf_params) -> int:
+    return int(lib().tf_cache_workspace_bytes(ctypes.byref(p)))
+
+
+class QuantCache:
+    """Device memory of a cache in 4 or 8 bits (allocated through torch, empty); `desc` is the tf_cache
+    that the calls take."""
+
+    def __init__(self, p: tf_params, capacity: int, format: int, device="cuda:0"):
+        size = tf_cache_bytes(p, format, capacity)
+        if size == 0:
+            raise TokfiltError(TF_ERR_INVALID_ARG, "parameters, format or capacity of a cache")
+        self.k = torch.empty(size, dtype=torch.uint8, device=device)
+        self.v = torch.empty(size, dtype=torch.uint8, device=device)
+        self.len = torch.zeros(p.batch, dtype=torch.int32, device=device)
+        self.overflow = torch.zeros(p.batch, dtype=torch.int32, device=device)
+        self.desc = tf_cache(self.k.data_ptr(), self.v.data_ptr(), self.len.data_ptr(),
+                             self.overflow.data_ptr(), int(capacity), int(format))
+
+
 class DecodeBuffers:
     """Device memory of one decoding sequence: the state tf_decode_state describes, the
-    per-step outputs and the workspace (allocated through torch; nothing is computed here)."""
+    per-step outputs and the workspace (allocated through torch; nothing is computed here).
+    cache_format: 0 for caches of the step's type, else the tf_cache_format of tf_decode_step_q."""
 
-    def __init__(self, p: tf_params, capacity: int, device="cuda:0"):
+    def __init__(self, p: tf_params, capacity: int, device="cuda:0", cache_format: int = 0):
         B, Hq, Hkv, d = p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim
         dt = torch.float32 if p.dtype == TF_F32 else torch.bfloat16
         i32 = dict(dtype=torch.int32, device=device)
@@ -202,12 +274,18 @@ class DecodeBuffers:
         self.seen, self.skipped = torch.empty(B, **i32), torch.empty(B, **i32)
         self.cache_len, self.overflow = torch.empty(B, **i32), torch.empty(B, **i32)
         self.tau = torch.empty(B, dtype=torch.float32, device=device)
-        self.k_cache = torch.empty((B, Hkv, capacity, d), dtype=dt, device=device)
-        self.v_cache = torch.empty((B, Hkv, capacity, d), dtype=dt, device=device)
+        if cache_format:
+            size = tf_cache_bytes(p, cache_format, capacity)
+            self.k_cache = torch.empty(size, dtype=torch.uint8, device=device)
+            self.v_cache = torch.empty(size, dtype=torch.uint8, device=device)
+        else:
+            self.k_cache = torch.empty((B, Hkv, capacity, d), dtype=dt, device=device)
+            self.v_cache = torch.empty((B, Hkv, capacity, d), dtype=dt, device=device)
         self.o = torch.empty((B, Hq, d), dtype=dt, device=device)
         self.skip = torch.empty(B, dtype=torch.uint8, device=device)
         self.fused = torch.empty(B, dtype=torch.float32, device=device)
-        self.ws = torch.empty((tf_decode_workspace_bytes(p),), dtype=torch.uint8, device=device)
+        ws = tf_cache_workspace_bytes(p) if cache_format else tf_decode_workspace_bytes(p)
+        self.ws = torch.empty((ws,), dtype=torch.uint8, device=device)
         st = tf_decode_state()
         for name in ("anchor_k", "anchor_v", "seen", "skipped", "tau", "cache_len", "overflow",
                      "k_cache", "v_cache"):
@@ -235,6 +313,34 @@ class Context:
             self._h, ctypes.byref(p), float(eta), ctypes.byref(state), _ptr(q), _ptr(k), _ptr(v),
             _ptr(o), _ptr(skip), _ptr(fused), _ptr(ws),
             _bytes(ws), _stream(stream)))
+
+    def tf_decode_prefill_q(self, p, eta, tau0, state, format, Q, K, V, keep, kept_idx, count, fused, O,
+                            ws, stream=None):
+        self._check(lib().tf_decode_prefill_q(
+            self._h, ctypes.byref(p), float(eta), float(tau0), ctypes.byref(state), int(format),
+            _ptr(Q), _ptr(K), _ptr(V), _ptr(keep), _ptr(kept_idx), _ptr(count), _ptr(fused), _ptr(O),
+            _ptr(ws), _bytes(ws), _stream(stream)))
+
+    def tf_decode_step_q(self, p, eta, state, format, q, k, v, o, skip, fused, ws, stream=None):
+        self._check(lib().tf_decode_step_q(
+            self._h, ctypes.byref(p), float(eta), ctypes.byref(state), int(format), _ptr(q), _ptr(k),
+            _ptr(v), _ptr(o), _ptr(skip), _ptr(fused), _ptr(ws), _bytes(ws), _stream(stream)))
+
+    def tf_norm_rotate(self, p, rotary, Q, K, Q_out, K_out, stream=None):
+        self._check(lib().tf_norm_rotate(self._h, ctypes.byref(p), ctypes.byref(rotary), _ptr(Q),
+                                         _ptr(K), _ptr(Q_out), _ptr(K_out), _stream(stream)))
+
+    def tf_cache_write(self, p, cache, K, V, kept_idx, m, count, stream=None):
+        self._check(lib().tf_cache_write(self._h, ctypes.byref(p), ctypes.byref(cache), _ptr(K), _ptr(V),
+                                         _ptr(kept_idx), int(m), _ptr(count), _stream(stream)))
+
+    def tf_cache_read(self, p, cache, start, K, V, stream=None):
+        self._check(lib().tf_cache_read(self._h, ctypes.byref(p), ctypes.byref(cache), _ptr(start),
+                                        _ptr(K), _ptr(V), _stream(stream)))
+
+    def tf_cache_attend(self, p, cache, Q, O, count, ws, stream=None):
+        self._check(lib().tf_cache_attend(self._h, ctypes.byref(p), ctypes.byref(cache), _ptr(Q), _ptr(O),
+                                          _ptr(count), _ptr(ws), _bytes(ws), _stream(stream)))
 
     def __init__(self, device: int = 0):
         self._h = ctypes.c_void_p()

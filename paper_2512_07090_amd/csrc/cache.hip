@@ -1,0 +1,483 @@
+// A cache in 4 or 8 bits (the format: cache_format.h): rows quantised as they are written, read back, and
+// attended to by the new tokens of a sequence.
+#include <algorithm>
+#include <type_traits>
+
+#include "cache_format.h"
+#include "decode_device.h"
+#include "tf_kernels.h"
+
+namespace tf {
+
+namespace {
+
+constexpr int kPartStride = kDecodePartFloats;
+
+__device__ __forceinline__ void store8(uint16_t* p, const float* x)
+{
+    // (what a code stands for is exact in bf16)
+    uint4 r;
+    unsigned* w = reinterpret_cast<unsigned*>(&r);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(__float_as_uint(x[2 * i + 1]), __float_as_uint(x[2 * i]), 0x07060302u);
+    *reinterpret_cast<uint4*>(p) = r;
+}
+__device__ __forceinline__ void store8(float* p, const float* x)
+{
+    reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+// A workgroup takes one page of one (tensor, batch row, KV head): 16 lanes a row, four rows a lane.
+// It lives on memory bandwidth: a row's 256 (512) bytes are read 16 lanes side by side, all four rows of a lane
+// are requested before the first is used.
+template <typename T, int BITS>
+__global__ __launch_bounds__(256) void cache_write_kernel(const CacheWriteArgs a)
+{
+    const int w = blockIdx.x & 1, rest = blockIdx.x >> 1;
+    const int page_i = rest % a.pages, bh = rest / a.pages, b = bh / a.Hkv, h = bh % a.Hkv;
+    const int held = min(max(a.len[b], 0), a.capacity);
+    const int rows = min(a.count ? min(max(a.count[b], 0), a.m) : a.m, a.capacity - held);
+    const int page = held / kPageRows + page_i;
+    if (rows < 1 || page * kPageRows >= held + rows) return;
+    const T* const src = static_cast<const T*>(w ? a.V : a.K) + b * a.kvs[0] + h * a.kvs[1];
+    uint8_t* const dst = static_cast<uint8_t*>(w ? a.v : a.k) + ((long long)bh * a.cache_pages + page) * page_bytes<BITS>();
+    const int c = threadIdx.x & 15, grp = threadIdx.x >> 4;
+    float x[4][8];
+    bool there[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int i = page * kPageRows + 16 * u + grp - held;   // the i-th row that is written
+        there[u] = i >= 0 && i < rows;
+        const int j = min(max(i, 0), rows - 1);
+        // (a position outside of the sequence is the caller's mistake; it is not read from there)
+        const int t = a.kept_idx ? min(max(a.kept_idx[(long long)b * a.m + j], 0), a.n - 1) : j;
+        load8(src + t * a.kvs[2] + 8 * c, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) store_row8<BITS>(dst, 16 * u + grp, c, x[u], w, there[u]);
+}
+
+__global__ void cache_advance_kernel(int32_t* len, int32_t* overflow, const int32_t* count, int m, int capacity, int B)
+{
+    const int b = blockIdx.x * blockDim.x + threadIdx.x;
+    if (b >= B) return;
+    const int held = min(max(len[b], 0), capacity), rows = count ? min(max(count[b], 0), m) : m;
+    len[b] = held + min(rows, capacity - held);
+    if (overflow && rows > capacity - held) overflow[b] = 1;
+}
+
+// The reverse, rows start[b] .. start[b] + n - 1 of the cache.
+template <typename T, int BITS>
+__global__ __launch_bounds__(256) void cache_read_kernel(const CacheReadArgs a)
+{
+    const int w = blockIdx.x & 1, rest = blockIdx.x >> 1;
+    const int page_i = rest % a.pages, bh = rest / a.pages, b = bh / a.Hkv, h = bh % a.Hkv;
+    const int held = min(max(a.len[b], 0), a.capacity), from = a.start ? max(a.start[b], 0) : 0;
+    if (from >= held) return;
+    const int to = min(held, from + min(a.n, held - from)), page = from / kPageRows + page_i;
+    if (page * kPageRows >= to) return;
+    T* const dst = static_cast<T*>(w ? a.V : a.K) + b * a.kvs[0] + h * a.kvs[1];
+    const uint8_t* const src = static_cast<const uint8_t*>(w ? a.v : a.k) + ((long long)bh * a.cache_pages + page) * page_bytes<BITS>();
+    const int c = threadIdx.x & 15, grp = threadIdx.x >> 4;
+    unsigned code[4][BITS / 4];
+    int e[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {   // (a page is there as a whole)
+        const int row = 16 * u + grp;
+        const unsigned* at = reinterpret_cast<const unsigned*>(src + (w ? value_code_at<BITS>(row, c) : key_code_at<BITS>(row, c)));
+#pragma unroll
+        for (int i = 0; i < BITS / 4; ++i) code[u][i] = at[i];
+        e[u] = src[w ? value_scale_at<BITS>(row, c >> 2) : key_scale_at<BITS>(row, c >> 2)];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int slot = page * kPageRows + 16 * u + grp;
+        if (slot < from || slot >= to) continue;
+        float x[8];
+        values_of8<BITS>(code[u], exponent_scale(e[u]), x);
+        store8(dst + (slot - from) * a.kvs[2] + 8 * c, x);
+    }
+}
+
+// ---- attention -----------------------------------------------------------------------------
+// A column is one query of one head: token t, head g of the `ratio` that share a KV head, column t * ratio + g.
+// A workgroup takes 16 columns and one slice of the row's keys, its four waves a page of 64 keys each in turn.
+//   S^T = K Q^T   v_mfma_f32_16x16x32_bf16, A: 16 keys, B: the columns.  A lane holds a block of 32 columns of a
+//                 key (the contraction order is dealt out so that these are contiguous), with one scale.
+//   O^T += V^T P^T  A: eight columns of the eight keys whose weights the lane holds, transposed within the lane.
+// Codes become bf16 exactly.  Weights and queries in fp32 are sums of bf16 parts: fp32 queries three parts, exact,
+// and so their weights; behind bf16 queries two (2^-16 of a weight, an output is rounded to 2^-9).
+// (The scaled 4-bit product, which would take codes as they are, adds up with less than fp32: 1.5e-4 of the sum of
+// magnitudes was measured, and queries would have to be rounded to 8 bits.)
+// Parts of two values: three of them cut off, which is exact, or two rounded.
+template <int PARTS>
+__device__ __forceinline__ void split_pair(float a, float b, unsigned* w)
+{
+    static_assert(PARTS == 2 || PARTS == 3, "");
+    if constexpr (PARTS == 3) {
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) {
+            w[i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+            a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+            b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+        }
+    } else {
+        w[0] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)a, (__bf16)b});
+        w[1] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)(a - __uint_as_float(w[0] << 16)), (__bf16)(b - __uint_as_float(w[0] & 0xffff0000u))});
+    }
+}
+template <int PARTS>
+__device__ __forceinline__ void load_query(const uint16_t* p, bf16x8* f)
+{
+    static_assert(PARTS == 1, "bf16 queries are whole");
+    f[0] = *reinterpret_cast<const bf16x8*>(p);
+}
+template <int PARTS>
+__device__ __forceinline__ void load_query(const float* p, bf16x8* f)
+{
+    float x[8];
+    load8(p, x);
+    u32x4 r[PARTS];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        unsigned w[PARTS];
+        split_pair<PARTS>(x[2 * i], x[2 * i + 1], w);
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) r[k][i] = w[k];
+    }
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) f[k] = __builtin_bit_cast(bf16x8, r[k]);
+}
+
+template <typename T, int BITS>
+__global__ __launch_bounds__(256, 2) void cache_attend_kernel(const CacheAttendArgs a)
+{
+    constexpr int kQ = sizeof(T) == 2 ? 1 : 3, kP = sizeof(T) == 2 ? 2 : 3;   // bf16 parts of a query, of a weight
+    constexpr int kRaw = BITS / 4;                                            // 16-byte loads of a lane and tile
+    constexpr int kRow = kHeadDim + 4;
+    __shared__ __attribute__((aligned(16))) float o_part[4][16][kRow];
+    __shared__ float stat[4][16][2];
+    __shared__ float weight[16][kDecodeMaxSplit + 1];
+    __shared__ int drawn;
+    const int lane = threadIdx.x & 63, c16 = lane & 15, g4 = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int sp = blockIdx.x % a.n_split, tile = blockIdx.x / a.n_split % a.tiles;
+    const int bh = blockIdx.x / a.n_split / a.tiles, b = bh / a.Hkv, hk = bh % a.Hkv;
+    const int ratio = a.Hq / a.Hkv;
+    const int held = min(max(a.len[b], 0), a.capacity);
+    const int there = a.skip && a.skip[b] ? 0 : a.count ? min(max(a.count[b], 0), a.n) : a.n;   // queries of this row
+    // keys that query t sees (none: a zero row)
+    auto sees = [&](int t) { return t < there ? max(held - there + t + 1, 0) : 0; };
+    const int cols = min(16, a.n * ratio - tile * 16);
+    auto token = [&](int col) { return (tile * 16 + col) / ratio; };
+    const int first_t = token(0), last_t = min(token(cols - 1), there - 1);
+    const int keys = last_t < first_t ? 0 : sees(last_t);        // of any of the columns
+    T* const out = static_cast<T*>(a.o) + b * a.os[0];
+    auto out_row = [&](int col) {
+        const int q = tile * 16 + col;
+        return out + (hk * ratio + q % ratio) * a.os[1] + q / ratio * a.os[2];
+    };
+    // the slices of a row follow from its own length
+    const int chunk = max(kCacheSlice, ((held + a.n_split - 1) / a.n_split + kPageRows - 1) / kPageRows * kPageRows);
+    const int used = (keys + chunk - 1) / chunk;
+    if (sp >= used) {
+        if (used == 0 && sp == 0)
+            for (int i = threadIdx.x; i < cols * kHeadDim; i += 256) store_out(out_row(i / kHeadDim) + i % kHeadDim, 0.f);
+        return;
+    }
+    const int lo = sp * chunk, hi = min(keys, lo + chunk);
+    const int col = min(c16, cols - 1), my_keys = c16 < cols ? sees(token(col)) : 0;
+    const int all_see = sees(first_t);   // keys that every column sees
+
+    bf16x8 qf[kQ][4];
+    {
+        const int q = tile * 16 + col;
+        const T* const row = static_cast<const T*>(a.q) + b * a.qs[0] + (hk * ratio + q % ratio) * a.qs[1] + q / ratio * a.qs[2] + 32 * g4;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            bf16x8 f[kQ];
+            load_query<kQ>(row + 8 * s, f);
+#pragma unroll
+            for (int i = 0; i < kQ; ++i) qf[i][s] = f[i];
+        }
+    }
+    const long long row_at = (long long)bh * a.cache_pages * page_bytes<BITS>();
+    const uint8_t* const kb = static_cast<const uint8_t*>(a.k) + row_at;
+    const uint8_t* const vb = static_cast<const uint8_t*>(a.v) + row_at;
+
+    f32x4 acc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float mx = kLowest, sum = 0.f;
+    u32x4 k_raw[4][kRaw], v_raw[4][kRaw], v_scale;
+    unsigned k_scale;
+    auto request_k = [&](int j) {
+        const uint8_t* p = kb + (long long)(j / kPageRows) * page_bytes<BITS>();
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < kRaw; ++i) k_raw[t][i] = *reinterpret_cast<const u32x4*>(p + key_code_at<BITS>(16 * t + c16, 4 * g4) + 16 * i);
+        k_scale = *reinterpret_cast<const unsigned*>(p + page_codes<BITS>() + 4 * lane);
+    };
+    auto request_v = [&](int j) {
+        const uint8_t* p = vb + (long long)(j / kPageRows) * page_bytes<BITS>();
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < kRaw; ++i) v_raw[t][i] = *reinterpret_cast<const u32x4*>(p + value_code_at<BITS>(16 * t + 4 * g4, c16) + 16 * i);
+        v_scale = *reinterpret_cast<const u32x4*>(p + page_codes<BITS>() + (4 * g4 + (c16 >> 2)) * 16);
+    };
+    int j = lo + kPageRows * wave;
+    if (j < hi) { request_k(j); request_v(j); }
+    for (; j < hi; j += 4 * kPageRows) {
+        float s[16];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const float scale = exponent_scale((k_scale >> (8 * t)) & 0xff);
+            f32x4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = 0; st < 4; ++st) {
+                unsigned code[BITS / 4];
+#pragma unroll
+                for (int i = 0; i < BITS / 4; ++i) code[i] = k_raw[t][(BITS / 4 * st + i) / 4][(BITS / 4 * st + i) % 4];
+                u32x4 f;
+                unsigned pair[4];
+                bf16_of8<BITS>(code, scale, pair);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f[i] = pair[i];
+#pragma unroll
+                for (int i = 0; i < kQ; ++i) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), qf[i][st], d, 0, 0, 0);
+            }
+#pragma unroll
+            for (int v = 0; v < 4; ++v) s[4 * t + v] = d[v] * a.scale_log2e;
+        }
+        const bool more = j + 4 * kPageRows < hi;
+        if (more) request_k(j + 4 * kPageRows);
+        if (j + kPageRows > all_see) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    if (j + 16 * t + 4 * g4 + v >= my_keys) s[4 * t + v] = kLowest;
+        }
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        top = wave_group_max(top);
+        if (__any(top > mx)) {
+            const float m_new = fmaxf(mx, top), down = __builtin_amdgcn_exp2f(mx - m_new);
+            mx = m_new;
+            sum *= down;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] *= down;
+        }
+        // keys behind the last: whatever lies there, their weights are zero and so are their values
+        const bool clear = j + kPageRows > hi;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            u32x4 pf[kP];
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(s[8 * h + e] - mx), p1 = __builtin_amdgcn_exp2f(s[8 * h + e + 1] - mx);
+                sum += p0 + p1;
+                unsigned w[kP];
+                split_pair<kP>(p0, p1, w);
+#pragma unroll
+                for (int i = 0; i < kP; ++i) pf[i][e / 2] = w[i];
+            }
+            unsigned val[8][4];   // eight columns of the lane's eight keys
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int t = 2 * h + e / 4, k = e % 4;
+                unsigned code[BITS / 4];
+#pragma unroll
+                for (int i = 0; i < BITS / 4; ++i) code[i] = v_raw[t][(BITS / 4 * k + i) / 4][(BITS / 4 * k + i) % 4];
+                unsigned ex = (v_scale[t] >> (8 * k)) & 0xff;
+                if (clear && j + 16 * t + 4 * g4 + k >= hi) {
+                    ex = 127;
+#pragma unroll
+                    for (int i = 0; i < BITS / 4; ++i) code[i] = 0;
+                }
+                bf16_of8<BITS>(code, exponent_scale(ex), val[e]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                u32x4 t;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] = __builtin_amdgcn_perm(val[2 * e + 1][i / 2], val[2 * e][i / 2], i & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                for (int k = 0; k < kP; ++k)
+                    acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t), __builtin_bit_cast(bf16x8, pf[k]), acc[i], 0, 0, 0);
+            }
+        }
+        if (more) request_v(j + 4 * kPageRows);
+    }
+
+    // the four waves' results through LDS (register v of product i is column 8 (4 g4 + v) + i)
+    sum = wave_group_sum(sum);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        float* dst = &o_part[wave][c16][8 * (4 * g4 + v)];
+        *reinterpret_cast<f32x4*>(dst) = f32x4{acc[0][v], acc[1][v], acc[2][v], acc[3][v]};
+        *reinterpret_cast<f32x4*>(dst + 4) = f32x4{acc[4][v], acc[5][v], acc[6][v], acc[7][v]};
+    }
+    if (lane < 16) { stat[wave][lane][0] = mx; stat[wave][lane][1] = sum; }
+    __syncthreads();
+    constexpr int kPairs = kPartStride / 2;   // the last one: running max, sum
+    float* const part0 = a.part + ((long long)bh * a.tiles + tile) * a.n_split * 16 * kPartStride;   // [slice][column]
+    for (int i = threadIdx.x; i < cols * kPairs; i += 256) {
+        const int q = i / kPairs, c = 2 * (i - q * kPairs);
+        float m_all = kLowest;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m_all = fmaxf(m_all, stat[w][q][0]);
+        Float2 v = {0.f, 0.f};
+        float den = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float wt = __builtin_amdgcn_exp2f(stat[w][q][0] - m_all);
+            den = fmaf(stat[w][q][1], wt, den);
+            if (c == kHeadDim) continue;
+            v.x = fmaf(o_part[w][q][c], wt, v.x);
+            v.y = fmaf(o_part[w][q][c + 1], wt, v.y);
+        }
+        if (c == kHeadDim) v = {m_all, den};
+        if (used > 1) put_shared(part0 + ((long long)sp * 16 + q) * kPartStride + c, v);
+        else if (c < kHeadDim) {
+            const bool some = sees(token(q)) > 0;
+            store_out(out_row(q) + c, some ? v.x / den : 0.f);
+            store_out(out_row(q) + c + 1, some ? v.y / den : 0.f);
+        }
+    }
+    if (used == 1) return;
+
+    // the workgroup that draws the last ticket of its columns merges the slices
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) drawn = __hip_atomic_fetch_add(a.tickets + bh * a.tiles + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (drawn != used - 1) return;
+    for (int q = wave; q < cols; q += 4) {
+        Float2 own = {kLowest, 0.f};
+        if (lane < used) own = get_shared(part0 + ((long long)lane * 16 + q) * kPartStride + kHeadDim);
+        float m_all = own.x;
+#pragma unroll
+        for (int step = 1; step < 64; step *= 2) m_all = fmaxf(m_all, __shfl_xor(m_all, step));
+        const float wt = __builtin_amdgcn_exp2f(own.x - m_all);
+        float den = own.y * wt;
+#pragma unroll
+        for (int step = 1; step < 64; step *= 2) den += __shfl_xor(den, step);
+        weight[q][lane] = wt;
+        if (lane == 0) weight[q][kDecodeMaxSplit] = den;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < cols * (kHeadDim / 2); i += 256) {
+        const int q = i / (kHeadDim / 2), c = 2 * (i % (kHeadDim / 2));
+        Float2 num = {0.f, 0.f};
+        for (int l = 0; l < used; l += 8) {
+            Float2 x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = get_shared(part0 + ((long long)min(l + u, used - 1) * 16 + q) * kPartStride + c);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float wt = l + u < used ? weight[q][l + u] : 0.f;
+                num.x = fmaf(x[u].x, wt, num.x);
+                num.y = fmaf(x[u].y, wt, num.y);
+            }
+        }
+        const float den = weight[q][kDecodeMaxSplit];
+        const bool some = sees(token(q)) > 0;
+        store_out(out_row(q) + c, some ? num.x / den : 0.f);
+        store_out(out_row(q) + c + 1, some ? num.y / den : 0.f);
+    }
+}
+
+__global__ void clear_tickets_kernel(int32_t* tickets, int n)
+{
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i < n) tickets[i] = 0;
+}
+
+}  // namespace
+
+size_t cache_bytes(int bits, long long caches, int capacity)
+{
+    const size_t pages = ((size_t)capacity + kPageRows - 1) / kPageRows;
+    return (size_t)caches * pages * (bits == 4 ? page_bytes<4>() : page_bytes<8>());
+}
+
+int32_t* cache_tickets(float* part, long long tiles, int n_split)
+{
+    return n_split > 1 ? (int32_t*)(part + tiles * n_split * 16 * kPartStride) : nullptr;
+}
+
+int cache_split(int B, int Hq, int Hkv, int n, int capacity, int n_cu)
+{
+    const long long tiles = (long long)B * Hkv * (((long long)n * (Hq / Hkv) + 15) / 16);
+    const long long most = std::min<long long>(kDecodeMaxSplit, (capacity + kCacheSlice - 1) / kCacheSlice);
+    return (int)std::min(std::max(2ll * n_cu / tiles, 1ll), most);
+}
+
+size_t cache_scratch_bytes(int B, int Hq, int Hkv, int n, int n_cu)
+{
+    const size_t tiles = (size_t)B * Hkv * (((size_t)n * (Hq / Hkv) + 15) / 16);
+    const int split = cache_split(B, Hq, Hkv, n, 1 << 30, n_cu);
+    return split == 1 ? 0 : tiles * (split * 16 * kPartStride + 1) * sizeof(float);
+}
+
+hipError_t launch_cache_write(const CacheWriteArgs& in, int dtype, int bits, hipStream_t s)
+{
+    CacheWriteArgs a = in;
+    a.pages = (a.m + kPageRows - 2) / kPageRows + 1;   // of a.m rows behind any others
+    const unsigned grid = (unsigned)(2ll * a.pages * a.B * a.Hkv);
+    if (dtype == 0) {
+        if (bits == 4) cache_write_kernel<float, 4><<<dim3(grid), dim3(256), 0, s>>>(a);
+        else cache_write_kernel<float, 8><<<dim3(grid), dim3(256), 0, s>>>(a);
+    } else {
+        if (bits == 4) cache_write_kernel<uint16_t, 4><<<dim3(grid), dim3(256), 0, s>>>(a);
+        else cache_write_kernel<uint16_t, 8><<<dim3(grid), dim3(256), 0, s>>>(a);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    cache_advance_kernel<<<dim3((unsigned)((a.B + 255) / 256)), dim3(256), 0, s>>>(a.len, a.overflow, a.count, a.m, a.capacity, a.B);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_read(const CacheReadArgs& in, int dtype, int bits, hipStream_t s)
+{
+    CacheReadArgs a = in;
+    a.pages = (a.n + kPageRows - 2) / kPageRows + 1;
+    const unsigned grid = (unsigned)(2ll * a.pages * a.B * a.Hkv);
+    if (dtype == 0) {
+        if (bits == 4) cache_read_kernel<float, 4><<<dim3(grid), dim3(256), 0, s>>>(a);
+        else cache_read_kernel<float, 8><<<dim3(grid), dim3(256), 0, s>>>(a);
+    } else {
+        if (bits == 4) cache_read_kernel<uint16_t, 4><<<dim3(grid), dim3(256), 0, s>>>(a);
+        else cache_read_kernel<uint16_t, 8><<<dim3(grid), dim3(256), 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_attend(const CacheAttendArgs& in, int dtype, int bits, bool clear, hipStream_t s)
+{
+    CacheAttendArgs a = in;
+    a.tiles = (int)(((long long)a.n * (a.Hq / a.Hkv) + 15) / 16);
+    const long long tiles = (long long)a.B * a.Hkv * a.tiles;
+    a.tickets = cache_tickets(a.part, tiles, a.n_split);
+    if (clear && a.n_split > 1) {
+        clear_tickets_kernel<<<dim3((unsigned)((tiles + 255) / 256)), dim3(256), 0, s>>>(a.tickets, (int)tiles);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const unsigned grid = (unsigned)(tiles * a.n_split);
+    if (dtype == 0) {
+        if (bits == 4) cache_attend_kernel<float, 4><<<dim3(grid), dim3(256), 0, s>>>(a);
+        else cache_attend_kernel<float, 8><<<dim3(grid), dim3(256), 0, s>>>(a);
+    } else {
+        if (bits == 4) cache_attend_kernel<uint16_t, 4><<<dim3(grid), dim3(256), 0, s>>>(a);
+        else cache_attend_kernel<uint16_t, 8><<<dim3(grid), dim3(256), 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace tf

@@ -6,6 +6,8 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "cache_format.h"
+#include "decode_device.h"
 #include "tf_kernels.h"
 
 namespace tf {
@@ -14,30 +16,9 @@ namespace {
 
 constexpr double kEpsCos = 1e-8;
 constexpr double kEpsVar = 1e-12;
-constexpr float kLowest = -1e30f;  // "no key yet": finite, so differences of two of them are 0
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kPartStride = kDecodePartFloats;  // partial result: 128 numerators, running max, sum
 
-// eight consecutive elements of a row as floats
-__device__ __forceinline__ void load8(const uint16_t* p, float* x)
-{
-    const uint4 r = *reinterpret_cast<const uint4*>(p);
-    const unsigned w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ void load8(const float* p, float* x)
-{
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-// the same in two steps: the bytes, and the floats they hold
+// eight floats of a row in two steps: the bytes, and the floats they hold
 struct Raw8 { float4 lo, hi; };
 __device__ __forceinline__ void unpack8(const Raw8& r, float* x)
 {
@@ -53,13 +34,6 @@ __device__ __forceinline__ void copy8(float* dst, const float* src)
     reinterpret_cast<float4*>(dst)[0] = reinterpret_cast<const float4*>(src)[0];
     reinterpret_cast<float4*>(dst)[1] = reinterpret_cast<const float4*>(src)[1];
 }
-__device__ __forceinline__ void store_out(uint16_t* p, float v)
-{
-    const unsigned u = __float_as_uint(v);
-    *p = (uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);  // round to nearest even
-}
-__device__ __forceinline__ void store_out(float* p, float v) { *p = v; }
-
 // two consecutive elements
 template <typename T> struct Raw2;
 template <> struct Raw2<uint16_t> { typedef unsigned type; };
@@ -123,12 +97,12 @@ __device__ __forceinline__ double wave_sum(double v)
     return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
 }
 
-template <typename T>
+template <typename T, int BITS>
 __device__ __forceinline__ void score_row(
     const T* __restrict__ k, const T* __restrict__ v, double* __restrict__ anchor_k,
     double* __restrict__ anchor_v, int32_t* __restrict__ seen, int32_t* __restrict__ skipped,
     float* __restrict__ tau, int32_t* __restrict__ cache_len, int32_t* __restrict__ overflow,
-    T* __restrict__ k_cache, T* __restrict__ v_cache, int capacity, int Hkv, int ema, double gamma,
+    void* __restrict__ k_cache, void* __restrict__ v_cache, int capacity, int Hkv, int ema, double gamma,
     int inclusive, int fusion, int warmup, float target, float eta,
     uint8_t* __restrict__ skip_out, float* __restrict__ fused_out, int32_t* __restrict__ tickets,
     int n_tickets)
@@ -230,10 +204,29 @@ __device__ __forceinline__ void score_row(
     for (int pr = grp; pr < 2 * Hkv; pr += n_grp) {
         const int w = pr >= Hkv, h = pr - w * Hkv;
         const T* src = (w ? v : k) + ((long long)b * Hkv + h) * kHeadDim + 2 * l16;
-        T* dst = (w ? v_cache : k_cache) + (((long long)b * Hkv + h) * capacity + slot) * kHeadDim + 2 * l16;
+        void* const cache = w ? v_cache : k_cache;
+        if constexpr (BITS == 0) {
+            T* dst = (T*)cache + (((long long)b * Hkv + h) * capacity + slot) * kHeadDim + 2 * l16;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<Pair*>(dst + 32 * i) = pr == grp ? first[i] : *reinterpret_cast<const Pair*>(src + 32 * i);
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<Pair*>(dst + 32 * i) = pr == grp ? first[i] : *reinterpret_cast<const Pair*>(src + 32 * i);
+        } else {
+            // two of the 32 columns of each block a lane, as they were read
+            const int pages = (capacity + kPageRows - 1) / kPageRows, row = slot % kPageRows;
+            uint8_t* const page = (uint8_t*)cache + (((long long)b * Hkv + h) * pages + slot / kPageRows) * page_bytes<BITS>();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float x[2];
+                unpack2(pr == grp ? first[i] : *reinterpret_cast<const Pair*>(src + 32 * i), x);
+                const int e = block_exponent<BITS>(row16_max(fmaxf(fabsf(x[0]), fabsf(x[1]))));
+                const unsigned code = codes_of2<BITS>(x[0], x[1], exponent_scale(e));
+                const int c = 4 * i + (l16 >> 2);   // eight columns 8 c, of which this lane has the pair l16 % 4
+                uint8_t* const at = page + (w ? value_code_at<BITS>(row, c) : key_code_at<BITS>(row, c)) + (l16 & 3) * (BITS / 4);
+                if constexpr (BITS == 4) *at = (uint8_t)code;
+                else *reinterpret_cast<uint16_t*>(at) = (uint16_t)code;
+                if (l16 == 0) page[w ? value_scale_at<BITS>(row, i) : key_scale_at<BITS>(row, i)] = (uint8_t)e;
+            }
+        }
     }
 }
 #pragma clang fp contract(fast)
@@ -247,7 +240,7 @@ template <typename T> struct ScoreArgs {
     int32_t *seen, *skipped;
     float* tau;
     int32_t *cache_len, *overflow;
-    T *k_cache, *v_cache;
+    void *k_cache, *v_cache;
     int capacity, Hkv, ema;
     double gamma;
     int inclusive, fusion, warmup;
@@ -257,41 +250,12 @@ template <typename T> struct ScoreArgs {
     int32_t* tickets;
     int n_tickets;
 };
-template <typename T>
+template <typename T, int BITS>
 __global__ __launch_bounds__(1024) void decode_score_kernel(const ScoreArgs<T> a)
 {
-    score_row<T>(a.k, a.v, a.anchor_k, a.anchor_v, a.seen, a.skipped, a.tau, a.cache_len, a.overflow, a.k_cache, a.v_cache,
+    score_row<T, BITS>(a.k, a.v, a.anchor_k, a.anchor_v, a.seen, a.skipped, a.tau, a.cache_len, a.overflow, a.k_cache, a.v_cache,
                  a.capacity, a.Hkv, a.ema, a.gamma, a.inclusive, a.fusion, a.warmup, a.target, a.eta, a.skip_out,
                  a.fused_out, a.tickets, a.n_tickets);
-}
-
-// sum over the four lanes that share lane % 16
-__device__ __forceinline__ float wave_group_sum(float v)
-{
-    const FloatPair a = swap16(v, v);
-    v = a.first + a.second;
-    const FloatPair b = swap32(v, v);
-    return b.first + b.second;
-}
-__device__ __forceinline__ float wave_group_max(float v)
-{
-    const FloatPair a = swap16(v, v);
-    v = fmaxf(a.first, a.second);
-    const FloatPair b = swap32(v, v);
-    return fmaxf(b.first, b.second);
-}
-
-// Two floats to or from memory past the caches that are not shared between the dies (relaxed, device
-// scope): written and read this way, a partial result needs no cache to be written back or
-// invalidated on its way from one workgroup to another.
-struct Float2 { float x, y; };
-__device__ __forceinline__ void put_shared(float* p, Float2 v)
-{
-    __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), __builtin_bit_cast(unsigned long long, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ Float2 get_shared(const float* p)
-{
-    return __builtin_bit_cast(Float2, __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 
 // Behind a slice's partial result, which the workgroup has just written: the workgroup that draws the last
@@ -738,12 +702,12 @@ __global__ __launch_bounds__(256, 2) void decode_attend_bf16_kernel(const Attend
 // 16 groups of 16 lanes.
 // The workgroups behind those `anchors` copy 64 kept rows of K and V each, in order, into the caches and
 // set the controller's counters (5 us when they were a launch of their own; neither part fills the chip).
-template <typename T, int LANES>
+template <typename T, int LANES, int BITS>
 __global__ __launch_bounds__(1024) void decode_seed_kernel(
     const T* __restrict__ K, const T* __restrict__ V, double* __restrict__ anchor_k,
     double* __restrict__ anchor_v, int Hkv, int n, long long s_b, long long s_h, long long s_t,
     double g, double weight, int window, int anchors, const int32_t* __restrict__ kept_idx,
-    const int32_t* __restrict__ count, T* __restrict__ k_cache, T* __restrict__ v_cache,
+    const int32_t* __restrict__ count, void* __restrict__ k_cache, void* __restrict__ v_cache,
     int32_t* __restrict__ seen, int32_t* __restrict__ skipped, int32_t* __restrict__ cache_len,
     int32_t* __restrict__ overflow, int capacity)
 {
@@ -757,9 +721,19 @@ __global__ __launch_bounds__(1024) void decode_seed_kernel(
         const int i = rb * 64 + (threadIdx.x >> 4), c8 = threadIdx.x & 15;
         if (i >= m) return;
         const long long src = b * s_b + h * s_h + (long long)kept_idx[(long long)b * n + i] * s_t + c8 * 8;
-        const long long dst = ((long long)bh * capacity + i) * kHeadDim + c8 * 8;
-        copy8(k_cache + dst, K + src);
-        copy8(v_cache + dst, V + src);
+        if constexpr (BITS == 0) {
+            const long long dst = ((long long)bh * capacity + i) * kHeadDim + c8 * 8;
+            copy8((T*)k_cache + dst, K + src);
+            copy8((T*)v_cache + dst, V + src);
+        } else {
+            const int pages = (capacity + kPageRows - 1) / kPageRows;
+            const long long page = ((long long)bh * pages + i / kPageRows) * page_bytes<BITS>();
+            float x[8], y[8];
+            load8(K + src, x);
+            load8(V + src, y);
+            store_row8<BITS>((uint8_t*)k_cache + page, i % kPageRows, c8, x, false, true);
+            store_row8<BITS>((uint8_t*)v_cache + page, i % kPageRows, c8, y, true, true);
+        }
         return;
     }
     constexpr int kGroups = 1024 / LANES, kParts = 16 / LANES;   // row groups; workgroups per chain
@@ -826,12 +800,19 @@ hipError_t launch_decode_seed_t(const DecodeArgs& a, const T* K, const T* V, con
     // below one workgroup per two compute units a chain's columns are shared out
     const int anchors = chains < 128 ? 4 * chains : chains;
     const unsigned grid = (unsigned)anchors + (unsigned)((n + 63) / 64) * a.B * a.Hkv;
-#define TF_DECODE_SEED(LANES)                                                                     \
-    decode_seed_kernel<T, LANES><<<dim3(grid), dim3(1024), 0, s>>>(                               \
+#define TF_DECODE_SEED(LANES, BITS)                                                               \
+    decode_seed_kernel<T, LANES, BITS><<<dim3(grid), dim3(1024), 0, s>>>(                         \
         K, V, a.anchor_k, a.anchor_v, a.Hkv, n, kvs[0], kvs[1], kvs[2], g, wt, window, anchors, kept_idx, \
-        count, (T*)a.k_cache, (T*)a.v_cache, a.seen, a.skipped, a.cache_len, a.overflow, a.capacity)
-    if (chains < 128) TF_DECODE_SEED(4);
-    else TF_DECODE_SEED(16);
+        count, a.k_cache, a.v_cache, a.seen, a.skipped, a.cache_len, a.overflow, a.capacity)
+    if (chains < 128) {
+        if (a.bits == 0) TF_DECODE_SEED(4, 0);
+        else if (a.bits == 4) TF_DECODE_SEED(4, 4);
+        else TF_DECODE_SEED(4, 8);
+    } else {
+        if (a.bits == 0) TF_DECODE_SEED(16, 0);
+        else if (a.bits == 4) TF_DECODE_SEED(16, 4);
+        else TF_DECODE_SEED(16, 8);
+    }
 #undef TF_DECODE_SEED
     return hipGetLastError();
 }
@@ -845,9 +826,9 @@ hipError_t launch_decode_step_t(const DecodeArgs& a, const T* q, const T* k, con
     const int ratio = a.Hq / a.Hkv, parts = (ratio + g - 1) / g, groups = a.Hkv * parts;
     // tickets of the attention's workgroups behind the partial results
     int32_t* const tickets = (int32_t*)(a.part + (size_t)a.B * a.Hq * a.n_split * kDecodePartFloats);
-    decode_score_kernel<T><<<dim3(a.B), dim3(threads), 0, s>>>(ScoreArgs<T>{
+    decode_score_kernel<T, 0><<<dim3(a.B), dim3(threads), 0, s>>>(ScoreArgs<T>{
         k, v, a.anchor_k, a.anchor_v, a.seen, a.skipped, a.tau, a.cache_len, a.overflow,
-        (T*)a.k_cache, (T*)a.v_cache, a.capacity, a.Hkv, a.ema, a.gamma, a.inclusive, a.fusion, a.warmup,
+        a.k_cache, a.v_cache, a.capacity, a.Hkv, a.ema, a.gamma, a.inclusive, a.fusion, a.warmup,
         a.target, a.eta, a.skip, a.fused, tickets, a.n_split > 1 ? groups : 0});
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -874,6 +855,32 @@ hipError_t launch_decode_step_t(const DecodeArgs& a, const T* q, const T* k, con
     else TF_DECODE_ATTEND(1, true);
 #undef TF_DECODE_ATTEND
     return hipGetLastError();
+}
+
+// The step over a cache in 4 or 8 bits: the same scoring, which quantises a kept token's rows as it writes them,
+// then the attention of one token a row.
+template <typename T>
+hipError_t launch_decode_step_bits_t(const DecodeArgs& a, const T* q, const T* k, const T* v, T* o, hipStream_t s)
+{
+    const int threads = std::min(1024, (32 * a.Hkv + 63) / 64 * 64);
+    const int tiles = a.Hkv * ((a.Hq / a.Hkv + 15) / 16);   // of a batch row, a ticket each
+    int32_t* const tickets = cache_tickets(a.part, a.B * tiles, a.n_split);
+    const ScoreArgs<T> score{k, v, a.anchor_k, a.anchor_v, a.seen, a.skipped, a.tau, a.cache_len, a.overflow,
+                             a.k_cache, a.v_cache, a.capacity, a.Hkv, a.ema, a.gamma, a.inclusive, a.fusion, a.warmup,
+                             a.target, a.eta, a.skip, a.fused, tickets, a.n_split > 1 ? tiles : 0};
+    if (a.bits == 4) decode_score_kernel<T, 4><<<dim3(a.B), dim3(threads), 0, s>>>(score);
+    else decode_score_kernel<T, 8><<<dim3(a.B), dim3(threads), 0, s>>>(score);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    CacheAttendArgs c = {};
+    c.q = q; c.k = a.k_cache; c.v = a.v_cache; c.o = o;
+    c.len = a.cache_len; c.skip = a.skip; c.part = a.part;
+    c.B = a.B; c.Hq = a.Hq; c.Hkv = a.Hkv; c.n = 1; c.capacity = a.capacity;
+    c.cache_pages = (a.capacity + kPageRows - 1) / kPageRows; c.n_split = a.n_split;
+    c.scale_log2e = a.scale * 1.4426950408889634f;
+    c.qs[0] = c.os[0] = (long long)a.Hq * kHeadDim;
+    c.qs[1] = c.os[1] = c.qs[2] = c.os[2] = kHeadDim;
+    return launch_cache_attend(c, sizeof(T) == 2, a.bits, false, s);
 }
 
 }  // namespace
@@ -969,6 +976,10 @@ hipError_t launch_decode_seed(const DecodeArgs& a, int dtype, const void* K, con
 hipError_t launch_decode_step(const DecodeArgs& a, int dtype, const void* q, const void* k,
                               const void* v, void* o, hipStream_t s)
 {
+    if (a.bits != 0) {
+        if (dtype == 0) return launch_decode_step_bits_t<float>(a, (const float*)q, (const float*)k, (const float*)v, (float*)o, s);
+        return launch_decode_step_bits_t<uint16_t>(a, (const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, (uint16_t*)o, s);
+    }
     if (dtype == 0)
         return launch_decode_step_t<float>(a, (const float*)q, (const float*)k, (const float*)v, (float*)o, s);
     return launch_decode_step_t<uint16_t>(a, (const uint16_t*)q, (const uint16_t*)k,

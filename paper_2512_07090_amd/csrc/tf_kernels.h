@@ -87,6 +87,7 @@ struct DecodeArgs {
     float* fused;                                   // out [B]
     float* part;                                    // scratch [B][Hq][n_split][kDecodePartFloats], tickets
     int n_few, n_split;                             // 1 .. decode_split()
+    int bits;                                       // of the caches: 0: of the step's type, 4, 8 (cache_format.h)
 };
 struct DecodeSplit { int few, most; };              // slices of a row; of one of kDecodeLongSlice * most keys or more (bf16)
 int decode_heads_per_wg(bool bf16, int B, int Hq, int Hkv);   // query heads one workgroup handles at most (they share a KV head)
@@ -103,6 +104,58 @@ hipError_t launch_decode_seed(const DecodeArgs& a, int dtype, const void* K, con
 // q, o: [B][Hq][128]; k, v: [B][Hkv][128]
 hipError_t launch_decode_step(const DecodeArgs& a, int dtype, const void* q, const void* k,
                               const void* v, void* o, hipStream_t s);
+
+// ---- norms of queries and keys and the position rotation ----------------------------------------
+struct NormRotateArgs {
+    const void *Q, *K;                              // either may be null
+    void *Q_out, *K_out;
+    const float *q_weight, *k_weight;               // [128], null: no norm
+    const double* freq;                             // [rot_dim / 2]
+    const int32_t *positions, *start;               // [B][n], [B], either may be null
+    float eps;
+    int rot_dim, interleaved;
+    int B, Hq, Hkv, n;
+    long long qs[3], kvs[3], os[3];
+};
+hipError_t launch_norm_rotate(const NormRotateArgs& a, int dtype, hipStream_t s);
+
+// ---- a cache in 4 or 8 bits (cache_format.h) ------------------------------------------------------
+struct CacheWriteArgs {
+    const void *K, *V;
+    void *k, *v;
+    int32_t *len, *overflow;                        // [B]; overflow may be null
+    const int32_t *kept_idx, *count;                // [B][m], [B], either may be null
+    int B, Hkv, n, m, capacity, cache_pages, pages;
+    long long kvs[3];
+};
+struct CacheReadArgs {
+    const void *k, *v;
+    void *K, *V;
+    const int32_t *len, *start;                     // [B]; start may be null
+    int B, Hkv, n, capacity, cache_pages, pages;
+    long long kvs[3];
+};
+struct CacheAttendArgs {
+    const void *q, *k, *v;
+    void* o;
+    const int32_t *len, *count;                     // [B]; count may be null
+    const uint8_t* skip;                            // [B], may be null: rows that get zeros
+    float* part;
+    int32_t* tickets;
+    int B, Hq, Hkv, n, tiles, capacity, cache_pages, n_split;
+    float scale_log2e;
+    long long qs[3], os[3];
+};
+constexpr int kCacheSlice = 128;                    // keys of a slice at least
+size_t cache_bytes(int bits, long long caches, int capacity);
+// slices of a row's keys for each 16 columns (queries x heads of a KV head), and what they need of a workspace
+int cache_split(int B, int Hq, int Hkv, int n, int capacity, int n_cu);
+size_t cache_scratch_bytes(int B, int Hq, int Hkv, int n, int n_cu = 256);
+int32_t* cache_tickets(float* part, long long tiles, int n_split);   // behind the partial results
+hipError_t launch_cache_write(const CacheWriteArgs& a, int dtype, int bits, hipStream_t s);
+hipError_t launch_cache_read(const CacheReadArgs& a, int dtype, int bits, hipStream_t s);
+// clear: the tickets are not known to be zero
+hipError_t launch_cache_attend(const CacheAttendArgs& a, int dtype, int bits, bool clear, hipStream_t s);
 
 // ---- measurement probes (not part of the path) ---------------------------------------------
 hipError_t launch_probe_stream_read(const void* src, size_t bytes, void* sink, int n_cu,
@@ -125,6 +178,15 @@ __device__ __forceinline__ float row16_sum(float v)
     v += dpp_mov<0x4E>(v);   // quad_perm [2,3,0,1]
     v += dpp_mov<0x141>(v);  // row_half_mirror
     v += dpp_mov<0x140>(v);  // row_mirror
+    return v;
+}
+
+__device__ __forceinline__ float row16_max(float v)
+{
+    v = fmaxf(v, dpp_mov<0xB1>(v));
+    v = fmaxf(v, dpp_mov<0x4E>(v));
+    v = fmaxf(v, dpp_mov<0x141>(v));
+    v = fmaxf(v, dpp_mov<0x140>(v));
     return v;
 }
 

@@ -210,8 +210,49 @@ tf_status decode_args(tf_ctx* ctx, const tf_params* p, const tf_decode_state* st
     a->gamma = (double)p->ema_gamma;
     a->target = (float)p->prune_ratio; a->eta = 0.f;
     a->scale = p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
-    a->skip = nullptr; a->fused = nullptr; a->part = nullptr; a->n_few = a->n_split = 1;
+    a->skip = nullptr; a->fused = nullptr; a->part = nullptr; a->n_few = a->n_split = 1; a->bits = 0;
     return TF_OK;
+}
+
+tf_status check_format(tf_ctx* ctx, int32_t format)
+{
+    if (format == TF_CACHE_FP4 || format == TF_CACHE_FP8) return TF_OK;
+    return fail(ctx, TF_ERR_INVALID_ARG, "unknown cache format");
+}
+
+// validation shared by the calls on a cache in 4 or 8 bits
+tf_status check_cache(tf_ctx* ctx, const tf_params* p, const tf_cache* c)
+{
+    if (!ctx) return TF_ERR_INVALID_ARG;
+    const char* why;
+    tf_status s = check_shape(p, &why);
+    if (s != TF_OK) return fail(ctx, s, "%s", why);
+    if (!c) return fail(ctx, TF_ERR_INVALID_ARG, "cache is NULL");
+    s = check_format(ctx, c->format);
+    if (s != TF_OK) return s;
+    if (!c->k || !c->v || !c->len) return fail(ctx, TF_ERR_INVALID_ARG, "k, v and len of the cache must not be NULL");
+    if (c->capacity < 1) return fail(ctx, TF_ERR_INVALID_ARG, "cache: capacity must be >= 1");
+    if (misaligned(c->k) || misaligned(c->v)) return fail(ctx, TF_ERR_INVALID_ARG, "caches must be 16-byte aligned");
+    if ((int64_t)p->batch * p->n_kv_heads * (int64_t)c->capacity > ((int64_t)1 << 40) / tf::kHeadDim)
+        return fail(ctx, TF_ERR_UNSUPPORTED, "cache too large");
+    return TF_OK;
+}
+
+tf_status use_device(tf_ctx* ctx)
+{
+    if (hipSetDevice(ctx->device) != hipSuccess) return fail(ctx, TF_ERR_DEVICE, "hipSetDevice(%d) failed", ctx->device);
+    return TF_OK;
+}
+
+int cache_pages(int32_t capacity) { return (int)(((int64_t)capacity + 63) / 64); }
+
+// an output whose rows share memory
+bool folded(const int64_t* stride, int batch, int heads) { return (batch > 1 && stride[0] == 0) || (heads > 1 && stride[1] == 0); }
+
+// workgroups of the calls that walk pages: one each for a page of a tensor's (batch row, KV head)
+bool too_many_pages(const tf_params* p, int rows)
+{
+    return 2 * ((int64_t)rows / 64 + 2) * p->batch * p->n_kv_heads >= ((int64_t)1 << 31);
 }
 
 }  // namespace
@@ -272,6 +313,50 @@ tf_status time_probe(tf_ctx* ctx, hipStream_t s, F launch, float* ms)
     (void)hipEventDestroy(e0);
     (void)hipEventDestroy(e1);
     return dev(ctx, e, "probe");
+}
+
+// the prompt of tf_decode_prefill and tf_decode_prefill_q (bits: of the caches, 0: of the prompt's type)
+tf_status prefill(tf_ctx* ctx, const tf_params* p, float eta, float tau0, const tf_decode_state* state, int bits,
+                  const void* Q, const void* K, const void* V, uint8_t* keep, int32_t* kept_idx, int32_t* count,
+                  float* fused, void* O, void* ws, size_t ws_bytes, void* stream)
+{
+    Workspace w;
+    tf_status st = enter(ctx, p, ws, ws_bytes, &w);
+    if (st != TF_OK) return st;
+    tf::DecodeArgs a;
+    st = decode_args(ctx, p, state, &a);
+    if (st != TF_OK) return st;
+    a.bits = bits;
+    if (state->capacity < p->seq)
+        return fail(ctx, TF_ERR_INVALID_ARG, "the caches hold %d rows, the prompt may keep %d", state->capacity, p->seq);
+    if ((int64_t)p->batch * p->n_kv_heads > 65535)
+        return fail(ctx, TF_ERR_UNSUPPORTED, "batch * n_kv_heads above 65535 is not supported by the hand-off");
+    if (!Q || !K || !V || !O || !keep || !kept_idx || !count || !fused)
+        return fail(ctx, TF_ERR_INVALID_ARG, "Q, K, V, O, keep, kept_idx, count and fused must not be NULL");
+    if (misaligned(Q) || misaligned(K) || misaligned(V) || misaligned(O))
+        return fail(ctx, TF_ERR_INVALID_ARG, "Q, K, V and O must be 16-byte aligned");
+    if (!(eta >= 0.f) || isinf(eta) || isnan(tau0) || isinf(tau0))
+        return fail(ctx, TF_ERR_INVALID_ARG, "eta must be finite and >= 0, tau0 finite");
+    if (p->seq > kMaxOnlineSeq)
+        return fail(ctx, TF_ERR_UNSUPPORTED, "the online decision counts skipped tokens in a float: seq above 2^24 is not supported");
+    const tf::Dims d = make_dims(p, p->seq);
+    hipStream_t s = (hipStream_t)stream;
+    char* base = (char*)ws;
+    float* sk = (float*)(base + w.sim_k);
+    float* sv = (float*)(base + w.sim_v);
+    st = dev(ctx, tf::launch_score(d, p->dtype, K, V, sk, sv, (float*)(base + w.seg_tot),
+                                   score_tensors(p), anchor_bits(p), p->ema_gamma, ctx->n_cu, s), "score launch");
+    if (st != TF_OK) return st;
+    st = dev(ctx, tf::launch_fuse(d, p->fusion, sk, sv, fused, s), "fuse launch");
+    if (st != TF_OK) return st;
+    // the threshold after the last prompt token goes straight into the state
+    st = dev(ctx, tf::launch_select_online(d, p->warmup, (float)p->prune_ratio, eta, tau0, fused, keep,
+                                           kept_idx, count, state->tau, s), "online decision launch");
+    if (st != TF_OK) return st;
+    st = run_attend(ctx, p, d, Q, K, V, kept_idx, O, s, -1, count);
+    if (st != TF_OK) return st;
+    return dev(ctx, tf::launch_decode_seed(a, p->dtype, K, V, kept_idx, count, p->seq, d.kvs, s),
+               "decode state hand-off launch");
 }
 
 }  // namespace
@@ -479,42 +564,7 @@ tf_status tf_decode_prefill(tf_ctx* ctx, const tf_params* p, float eta, float ta
                             const void* V, uint8_t* keep, int32_t* kept_idx, int32_t* count,
                             float* fused, void* O, void* ws, size_t ws_bytes, void* stream)
 {
-    Workspace w;
-    tf_status st = enter(ctx, p, ws, ws_bytes, &w);
-    if (st != TF_OK) return st;
-    tf::DecodeArgs a;
-    st = decode_args(ctx, p, state, &a);
-    if (st != TF_OK) return st;
-    if (state->capacity < p->seq)
-        return fail(ctx, TF_ERR_INVALID_ARG, "the caches hold %d rows, the prompt may keep %d", state->capacity, p->seq);
-    if ((int64_t)p->batch * p->n_kv_heads > 65535)
-        return fail(ctx, TF_ERR_UNSUPPORTED, "batch * n_kv_heads above 65535 is not supported by the hand-off");
-    if (!Q || !K || !V || !O || !keep || !kept_idx || !count || !fused)
-        return fail(ctx, TF_ERR_INVALID_ARG, "Q, K, V, O, keep, kept_idx, count and fused must not be NULL");
-    if (misaligned(Q) || misaligned(K) || misaligned(V) || misaligned(O))
-        return fail(ctx, TF_ERR_INVALID_ARG, "Q, K, V and O must be 16-byte aligned");
-    if (!(eta >= 0.f) || isinf(eta) || isnan(tau0) || isinf(tau0))
-        return fail(ctx, TF_ERR_INVALID_ARG, "eta must be finite and >= 0, tau0 finite");
-    if (p->seq > kMaxOnlineSeq)
-        return fail(ctx, TF_ERR_UNSUPPORTED, "the online decision counts skipped tokens in a float: seq above 2^24 is not supported");
-    const tf::Dims d = make_dims(p, p->seq);
-    hipStream_t s = (hipStream_t)stream;
-    char* base = (char*)ws;
-    float* sk = (float*)(base + w.sim_k);
-    float* sv = (float*)(base + w.sim_v);
-    st = dev(ctx, tf::launch_score(d, p->dtype, K, V, sk, sv, (float*)(base + w.seg_tot),
-                                   score_tensors(p), anchor_bits(p), p->ema_gamma, ctx->n_cu, s), "score launch");
-    if (st != TF_OK) return st;
-    st = dev(ctx, tf::launch_fuse(d, p->fusion, sk, sv, fused, s), "fuse launch");
-    if (st != TF_OK) return st;
-    // the threshold after the last prompt token goes straight into the state
-    st = dev(ctx, tf::launch_select_online(d, p->warmup, (float)p->prune_ratio, eta, tau0, fused, keep,
-                                           kept_idx, count, state->tau, s), "online decision launch");
-    if (st != TF_OK) return st;
-    st = run_attend(ctx, p, d, Q, K, V, kept_idx, O, s, -1, count);
-    if (st != TF_OK) return st;
-    return dev(ctx, tf::launch_decode_seed(a, p->dtype, K, V, kept_idx, count, p->seq, d.kvs, s),
-               "decode state hand-off launch");
+    return prefill(ctx, p, eta, tau0, state, 0, Q, K, V, keep, kept_idx, count, fused, O, ws, ws_bytes, stream);
 }
 
 tf_status tf_decode_step(tf_ctx* ctx, const tf_params* p, float eta, const tf_decode_state* state,
@@ -548,6 +598,164 @@ tf_status tf_decode_step(tf_ctx* ctx, const tf_params* p, float eta, const tf_de
     a.n_few = std::min(split.few, held);
     // (a cache without room for a long row has no use for a long row's slices)
     a.n_split = state->capacity >= split.most * tf::kDecodeLongSlice ? std::min(split.most, held) : a.n_few;
+    return dev(ctx, tf::launch_decode_step(a, p->dtype, q, k, v, o, (hipStream_t)stream), "decode step launch");
+}
+
+tf_status tf_norm_rotate(tf_ctx* ctx, const tf_params* p, const tf_rotary* r, const void* Q, const void* K,
+                         void* Q_out, void* K_out, void* stream)
+{
+    if (!ctx) return TF_ERR_INVALID_ARG;
+    const char* why;
+    tf_status st = check_shape(p, &why);
+    if (st != TF_OK) return fail(ctx, st, "%s", why);
+    if (!r) return fail(ctx, TF_ERR_INVALID_ARG, "the rotation's description is NULL");
+    if (!(r->eps > 0.f) || isinf(r->eps)) return fail(ctx, TF_ERR_INVALID_ARG, "eps must be finite and > 0");
+    if (r->rot_dim < 0 || r->rot_dim > tf::kHeadDim || r->rot_dim % 16 != 0)
+        return fail(ctx, TF_ERR_INVALID_ARG, "rot_dim must be a multiple of 16 in [0, 128]");
+    if ((r->interleaved != 0 && r->interleaved != 1) || r->reserved != 0)
+        return fail(ctx, TF_ERR_INVALID_ARG, "interleaved must be 0 or 1 and reserved 0");
+    if (r->rot_dim > 0 && !r->freq) return fail(ctx, TF_ERR_INVALID_ARG, "freq must not be NULL");
+    if (!Q != !Q_out || !K != !K_out || (!Q && !K))
+        return fail(ctx, TF_ERR_INVALID_ARG, "Q and Q_out, or K and K_out, must both be there or both be NULL");
+    if (misaligned(Q) || misaligned(K) || misaligned(Q_out) || misaligned(K_out))
+        return fail(ctx, TF_ERR_INVALID_ARG, "Q, K, Q_out and K_out must be 16-byte aligned");
+    if (Q && Q == Q_out)
+        for (int i = 0; i < 3; ++i)
+            if (p->q_stride[i] != p->o_stride[i])
+                return fail(ctx, TF_ERR_INVALID_ARG, "in place the strides of Q and of its output must be equal");
+    if ((Q && folded(p->o_stride, p->batch, p->n_q_heads)) || (K && folded(p->kv_stride, p->batch, p->n_kv_heads)))
+        return fail(ctx, TF_ERR_INVALID_ARG, "an output must not have a stride of 0");
+    st = use_device(ctx);
+    if (st != TF_OK) return st;
+    tf::NormRotateArgs a;
+    a.Q = Q; a.K = K; a.Q_out = Q_out; a.K_out = K_out;
+    a.q_weight = r->q_weight; a.k_weight = r->k_weight; a.freq = r->freq; a.positions = r->positions; a.start = r->start;
+    a.eps = r->eps; a.rot_dim = r->rot_dim; a.interleaved = r->interleaved;
+    a.B = p->batch; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.n = p->seq;
+    for (int i = 0; i < 3; ++i) { a.qs[i] = p->q_stride[i]; a.kvs[i] = p->kv_stride[i]; a.os[i] = p->o_stride[i]; }
+    return dev(ctx, tf::launch_norm_rotate(a, p->dtype, (hipStream_t)stream), "norm and rotation launch");
+}
+
+size_t tf_cache_bytes(const tf_params* p, int32_t format, int32_t capacity)
+{
+    const char* why;
+    if (check_shape(p, &why) != TF_OK || capacity < 1 || (format != TF_CACHE_FP4 && format != TF_CACHE_FP8)) return 0;
+    return tf::cache_bytes(format, (long long)p->batch * p->n_kv_heads, capacity);
+}
+
+size_t tf_cache_workspace_bytes(const tf_params* p)
+{
+    const char* why;
+    if (check_shape(p, &why) != TF_OK) return 0;
+    const size_t step = tf::cache_scratch_bytes(p->batch, p->n_q_heads, p->n_kv_heads, 1);
+    return align256(std::max({step, tf::cache_scratch_bytes(p->batch, p->n_q_heads, p->n_kv_heads, p->seq), (size_t)256}));
+}
+
+tf_status tf_cache_write(tf_ctx* ctx, const tf_params* p, const tf_cache* cache, const void* K, const void* V,
+                         const int32_t* kept_idx, int32_t m, const int32_t* count, void* stream)
+{
+    tf_status st = check_cache(ctx, p, cache);
+    if (st != TF_OK) return st;
+    if (!K || !V) return fail(ctx, TF_ERR_INVALID_ARG, "K and V must not be NULL");
+    if (misaligned(K) || misaligned(V)) return fail(ctx, TF_ERR_INVALID_ARG, "K and V must be 16-byte aligned");
+    if (m < 1 || m > p->seq) return fail(ctx, TF_ERR_INVALID_ARG, "m must be in [1, seq]");
+    if (too_many_pages(p, m)) return fail(ctx, TF_ERR_UNSUPPORTED, "too many rows for one call");
+    st = use_device(ctx);
+    if (st != TF_OK) return st;
+    tf::CacheWriteArgs a;
+    a.K = K; a.V = V; a.k = cache->k; a.v = cache->v; a.len = cache->len; a.overflow = cache->overflow;
+    a.kept_idx = kept_idx; a.count = count;
+    a.B = p->batch; a.Hkv = p->n_kv_heads; a.n = p->seq; a.m = m; a.capacity = cache->capacity;
+    a.cache_pages = cache_pages(cache->capacity); a.pages = 0;
+    for (int i = 0; i < 3; ++i) a.kvs[i] = p->kv_stride[i];
+    return dev(ctx, tf::launch_cache_write(a, p->dtype, cache->format, (hipStream_t)stream), "cache write launch");
+}
+
+tf_status tf_cache_read(tf_ctx* ctx, const tf_params* p, const tf_cache* cache, const int32_t* start, void* K,
+                        void* V, void* stream)
+{
+    tf_status st = check_cache(ctx, p, cache);
+    if (st != TF_OK) return st;
+    if (!K || !V) return fail(ctx, TF_ERR_INVALID_ARG, "K and V must not be NULL");
+    if (misaligned(K) || misaligned(V)) return fail(ctx, TF_ERR_INVALID_ARG, "K and V must be 16-byte aligned");
+    if (folded(p->kv_stride, p->batch, p->n_kv_heads)) return fail(ctx, TF_ERR_INVALID_ARG, "an output must not have a stride of 0");
+    if (too_many_pages(p, p->seq)) return fail(ctx, TF_ERR_UNSUPPORTED, "too many rows for one call");
+    st = use_device(ctx);
+    if (st != TF_OK) return st;
+    tf::CacheReadArgs a;
+    a.k = cache->k; a.v = cache->v; a.K = K; a.V = V; a.len = cache->len; a.start = start;
+    a.B = p->batch; a.Hkv = p->n_kv_heads; a.n = p->seq; a.capacity = cache->capacity;
+    a.cache_pages = cache_pages(cache->capacity); a.pages = 0;
+    for (int i = 0; i < 3; ++i) a.kvs[i] = p->kv_stride[i];
+    return dev(ctx, tf::launch_cache_read(a, p->dtype, cache->format, (hipStream_t)stream), "cache read launch");
+}
+
+tf_status tf_cache_attend(tf_ctx* ctx, const tf_params* p, const tf_cache* cache, const void* Q, void* O,
+                          const int32_t* count, void* ws, size_t ws_bytes, void* stream)
+{
+    tf_status st = check_cache(ctx, p, cache);
+    if (st != TF_OK) return st;
+    if (!Q || !O) return fail(ctx, TF_ERR_INVALID_ARG, "Q and O must not be NULL");
+    if (misaligned(Q) || misaligned(O)) return fail(ctx, TF_ERR_INVALID_ARG, "Q and O must be 16-byte aligned");
+    if (Q == O) return fail(ctx, TF_ERR_INVALID_ARG, "Q and O must not overlap");
+    if (folded(p->o_stride, p->batch, p->n_q_heads)) return fail(ctx, TF_ERR_INVALID_ARG, "an output must not have a stride of 0");
+    if (!ws || misaligned(ws)) return fail(ctx, TF_ERR_INVALID_ARG, "workspace must be a 16-byte aligned pointer");
+    const int n_cu = std::min(ctx->n_cu, 256);   // (workspaces are sized for 256)
+    const size_t need = tf::cache_scratch_bytes(p->batch, p->n_q_heads, p->n_kv_heads, p->seq, n_cu);
+    if (ws_bytes < need)
+        return fail(ctx, TF_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, need);
+    if ((int64_t)p->batch * p->n_kv_heads * (((int64_t)p->seq * (p->n_q_heads / p->n_kv_heads) + 15) / 16) >= ((int64_t)1 << 25))
+        return fail(ctx, TF_ERR_UNSUPPORTED, "too many queries for one call");
+    st = use_device(ctx);
+    if (st != TF_OK) return st;
+    tf::CacheAttendArgs a;
+    a.q = Q; a.k = cache->k; a.v = cache->v; a.o = O; a.len = cache->len; a.count = count; a.skip = nullptr;
+    a.part = (float*)ws; a.tickets = nullptr;
+    a.B = p->batch; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.n = p->seq; a.tiles = 0; a.capacity = cache->capacity;
+    a.cache_pages = cache_pages(cache->capacity);
+    a.n_split = tf::cache_split(p->batch, p->n_q_heads, p->n_kv_heads, p->seq, cache->capacity, n_cu);
+    a.scale_log2e = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim)) * 1.4426950408889634f;
+    for (int i = 0; i < 3; ++i) { a.qs[i] = p->q_stride[i]; a.os[i] = p->o_stride[i]; }
+    return dev(ctx, tf::launch_cache_attend(a, p->dtype, cache->format, true, (hipStream_t)stream), "cache attention launch");
+}
+
+tf_status tf_decode_prefill_q(tf_ctx* ctx, const tf_params* p, float eta, float tau0, const tf_decode_state* state,
+                              int32_t format, const void* Q, const void* K, const void* V, uint8_t* keep,
+                              int32_t* kept_idx, int32_t* count, float* fused, void* O, void* ws, size_t ws_bytes,
+                              void* stream)
+{
+    if (!ctx) return TF_ERR_INVALID_ARG;
+    const tf_status st = check_format(ctx, format);
+    if (st != TF_OK) return st;
+    return prefill(ctx, p, eta, tau0, state, format, Q, K, V, keep, kept_idx, count, fused, O, ws, ws_bytes, stream);
+}
+
+tf_status tf_decode_step_q(tf_ctx* ctx, const tf_params* p, float eta, const tf_decode_state* state, int32_t format,
+                           const void* q, const void* k, const void* v, void* o, uint8_t* skip, float* fused, void* ws,
+                           size_t ws_bytes, void* stream)
+{
+    if (!ctx) return TF_ERR_INVALID_ARG;
+    tf_status st = check_format(ctx, format);
+    if (st != TF_OK) return st;
+    tf::DecodeArgs a;
+    st = decode_args(ctx, p, state, &a);
+    if (st != TF_OK) return st;
+    if (!q || !k || !v || !o || !skip || !fused)
+        return fail(ctx, TF_ERR_INVALID_ARG, "q, k, v, o, skip and fused must not be NULL");
+    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(o))
+        return fail(ctx, TF_ERR_INVALID_ARG, "q, k, v and o must be 16-byte aligned");
+    if (!(eta >= 0.f) || isinf(eta)) return fail(ctx, TF_ERR_INVALID_ARG, "eta must be finite and >= 0");
+    if (!ws || misaligned(ws)) return fail(ctx, TF_ERR_INVALID_ARG, "workspace must be a 16-byte aligned pointer");
+    const int n_cu = std::min(ctx->n_cu, 256);
+    const size_t need = tf::cache_scratch_bytes(p->batch, p->n_q_heads, p->n_kv_heads, 1, n_cu);
+    if (ws_bytes < need)
+        return fail(ctx, TF_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, need);
+    a.bits = format;
+    a.eta = eta;
+    a.skip = skip;
+    a.fused = fused;
+    a.part = (float*)ws;
+    a.n_split = tf::cache_split(p->batch, p->n_q_heads, p->n_kv_heads, 1, state->capacity, n_cu);
     return dev(ctx, tf::launch_decode_step(a, p->dtype, q, k, v, o, (hipStream_t)stream), "decode step launch");
 }
 
