@@ -307,7 +307,8 @@ tf_status tf_decode_step(tf_ctx *ctx, const tf_params *p, float eta, const tf_de
  * included.  Position times frequency is formed and reduced to less than a turn in double, everything
  * else is fp32 with one rounding at the end, whatever the dtype. */
 typedef struct {
-    const float *q_weight, *k_weight; /* DEVICE [128] each; NULL: that tensor is not normalised */
+    const float *q_weight, *k_weight; /* DEVICE [128] each, 16-byte aligned; NULL: that tensor is not
+                                         normalised */
     const double *freq;               /* DEVICE [rot_dim / 2], radians per position (NULL if rot_dim is 0) */
     const int32_t *positions;         /* DEVICE [batch][seq], or NULL */
     const int32_t *start;             /* DEVICE [batch], or NULL */

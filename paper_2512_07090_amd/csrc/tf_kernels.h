@@ -114,7 +114,7 @@ struct NormRotateArgs {
     const int32_t *positions, *start;               // [B][n], [B], either may be null
     float eps;
     int rot_dim, interleaved;
-    int B, Hq, Hkv, n;
+    int B, Hq, Hkv, n, parts_q, parts;              // parts: workgroups for a token's heads
     long long qs[3], kvs[3], os[3];
 };
 hipError_t launch_norm_rotate(const NormRotateArgs& a, int dtype, hipStream_t s);

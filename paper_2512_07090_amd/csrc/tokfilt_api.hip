@@ -615,6 +615,8 @@ tf_status tf_norm_rotate(tf_ctx* ctx, const tf_params* p, const tf_rotary* r, co
     if ((r->interleaved != 0 && r->interleaved != 1) || r->reserved != 0)
         return fail(ctx, TF_ERR_INVALID_ARG, "interleaved must be 0 or 1 and reserved 0");
     if (r->rot_dim > 0 && !r->freq) return fail(ctx, TF_ERR_INVALID_ARG, "freq must not be NULL");
+    if (misaligned(r->q_weight) || misaligned(r->k_weight) || ((uintptr_t)r->freq & 7) != 0)
+        return fail(ctx, TF_ERR_INVALID_ARG, "weights must be 16-byte aligned and freq 8-byte aligned");
     if (!Q != !Q_out || !K != !K_out || (!Q && !K))
         return fail(ctx, TF_ERR_INVALID_ARG, "Q and Q_out, or K and K_out, must both be there or both be NULL");
     if (misaligned(Q) || misaligned(K) || misaligned(Q_out) || misaligned(K_out))

@@ -95,7 +95,7 @@ int main()
     auto rotate = [&](const tf_rotary* rr, const tf_params* pp, const void* q, const void* k, void* qo, void* ko) { return tf_norm_rotate(c, pp, rr, q, k, qo, ko, nullptr); };
     expect(nullptr, tf_norm_rotate(nullptr, &p, &r, Q, K, O, V, nullptr), inv, "rotate, no context");
     expect(c, rotate(nullptr, &p, Q, K, O, V), inv, "rotate, no description");
-    for (int i = 0; i < 9; ++i) {
+    for (int i = 0; i < 12; ++i) {
         tf_rotary x = r;
         if (i == 0) x.rot_dim = 8;
         if (i == 1) x.rot_dim = 144;
@@ -106,6 +106,9 @@ int main()
         if (i == 6) x.eps = INFINITY;
         if (i == 7) x.interleaved = 2;
         if (i == 8) x.reserved = 1;
+        if (i == 9) x.q_weight = (const float*)K + 1;
+        if (i == 10) x.k_weight = (const float*)K + 2;
+        if (i == 11) x.freq = (const double*)((const float*)K + 1);
         expect(c, rotate(&x, &p, Q, K, O, V), inv, "rotate, bad description");
     }
     expect(c, rotate(&r, &p, nullptr, nullptr, nullptr, nullptr), inv, "rotate, nothing");
