@@ -370,7 +370,10 @@ tf_status tf_cache_read(tf_ctx *ctx, const tf_params *p, const tf_cache *cache, 
  * Queries from count[b] on (padding), and any that see no row, get a zero output row.
  *   Q  in  p->q_stride, O  out  p->o_stride (must not overlap), count  DEVICE [batch], 0 .. seq, or NULL
  * Arithmetic: what the codes stand for enters exactly; fp32 softmax and accumulation; queries as they
- * are; weights to 2^-16 of themselves for TF_BF16 (the output is rounded to bf16), to fp32 for TF_F32.
+ * are.  Weights are fp32 for TF_F32; for TF_BF16, whose output is rounded to bf16, they are held to 2^-16 of
+ * themselves, or, in calls of so many queries that the arithmetic is what they wait for (batch * n_kv_heads
+ * * ceil(seq * n_q_heads / n_kv_heads / 16) of two per compute unit or more), rounded to bf16 once, as in
+ * tf_attend, and summed as rounded.
  * A row's results, rounding included, follow from its own queries, keys, len and count, `p` and
  * cache->capacity alone. */
 tf_status tf_cache_attend(tf_ctx *ctx, const tf_params *p, const tf_cache *cache, const void *Q, void *O,

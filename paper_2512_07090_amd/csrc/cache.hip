@@ -169,20 +169,26 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const CacheReadArgs a)
 
 // ---- attention -----------------------------------------------------------------------------
 // A column is one query of one head: token t, head g of the `ratio` that share a KV head, column t * ratio + g.
-// A workgroup takes 16 columns and one slice of the row's keys, its four waves a page of 64 keys each in turn.
+// A workgroup takes CT tiles of 16 columns and one slice of the row's keys, a wave a page of 64 keys at a time.
 //   S^T = K Q^T   v_mfma_f32_16x16x32_bf16, A: 16 keys, B: the columns.  A lane holds a block of 32 columns of a
 //                 key (the contraction order is dealt out so that these are contiguous), with one scale.
 //   O^T += V^T P^T  A: eight columns of the eight keys whose weights the lane holds, transposed within the lane.
-// Codes become bf16 exactly.  Weights and queries in fp32 are sums of bf16 parts: fp32 queries three parts, exact,
-// and so their weights; behind bf16 queries two (2^-16 of a weight, an output is rounded to 2^-9).
+// Codes become bf16 exactly, two an instruction.  fp32 queries and their weights are sums of three bf16 parts, which
+// is exact.  Behind bf16 queries weights are two parts (2^-16), or, where a call has many columns (CT = 2), rounded
+// to bf16 once as the batched attention does, numerator and denominator alike: with two parts 2 x 256 queries of 32
+// / 8 heads x 6000 keys took 85 us, 68 so.
 // (The scaled 4-bit product, which would take codes as they are, adds up with less than fp32: 1.5e-4 of the sum of
 // magnitudes was measured, and queries would have to be rounded to 8 bits.)
+// What bounds it: long caches the way of their bytes (8 x 32 heads x 8192 keys in 4 bits, 285 MB: 53 us, 5.3 TB/s),
+// many queries the instructions that convert and weigh (2 x 256 queries: 40.7 GFLOP at 0.59 PFLOP/s), short caches a
+// chain of latencies (32 / 8 heads x 500 keys: 6.7 us, of which a launch with one load takes 2.5).
 // Parts of two values: three of them cut off, which is exact, or two rounded.
 template <int PARTS>
 __device__ __forceinline__ void split_pair(float a, float b, unsigned* w)
 {
-    static_assert(PARTS == 2 || PARTS == 3, "");
-    if constexpr (PARTS == 3) {
+    if constexpr (PARTS == 1) {
+        w[0] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)a, (__bf16)b});
+    } else if constexpr (PARTS == 3) {
 #pragma unroll
         for (int i = 0; i < PARTS; ++i) {
             w[i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
@@ -217,66 +223,97 @@ __device__ __forceinline__ void load_query(const float* p, bf16x8* f)
     for (int k = 0; k < PARTS; ++k) f[k] = __builtin_bit_cast(bf16x8, r[k]);
 }
 
-template <typename T, int BITS>
-__global__ __launch_bounds__(256, 2) void cache_attend_kernel(const CacheAttendArgs a)
+template <typename T, int BITS, int CT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const CacheAttendArgs a)
 {
-    constexpr int kQ = sizeof(T) == 2 ? 1 : 3, kP = sizeof(T) == 2 ? 2 : 3;   // bf16 parts of a query, of a weight
+    constexpr int kQ = sizeof(T) == 2 ? 1 : 3, kP = sizeof(T) != 2 ? 3 : CT == 1 ? 2 : 1;   // bf16 parts of a query, of a weight
     constexpr int kRaw = BITS / 4;                                            // 16-byte loads of a lane and tile
-    constexpr int kRow = kHeadDim + 4;
-    __shared__ __attribute__((aligned(16))) float o_part[4][16][kRow];
-    __shared__ float stat[4][16][2];
-    __shared__ float weight[16][kDecodeMaxSplit + 1];
+    constexpr int kCols = 16 * CT, kThreads = 64 * WAVES, kRow = kHeadDim + 4;
+    __shared__ __attribute__((aligned(16))) float o_part[WAVES][kCols][kRow];
+    __shared__ float stat[WAVES][kCols][2];
+    __shared__ float weight[kCols][kDecodeMaxSplit + 1];
     __shared__ int drawn;
     const int lane = threadIdx.x & 63, c16 = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int sp = blockIdx.x % a.n_split, tile = blockIdx.x / a.n_split % a.tiles;
-    const int bh = blockIdx.x / a.n_split / a.tiles, b = bh / a.Hkv, hk = bh % a.Hkv;
+    // The tiles of a cache go to one die, whose L2 they then share: workgroups are dealt out to the dies in turn, so
+    // eight caches a time, one for each; what is left over of them is spread.
+    int at = blockIdx.x;
+    int bh = at / a.n_split / a.tiles;
+    if (a.tiles > 1) {
+        const int group = a.n_split * a.tiles, caches = a.B * a.Hkv;
+        if (const int eight = at / (8 * group); 8 * eight + 8 <= caches) {
+            bh = 8 * eight + at % 8;
+            at = at % (8 * group) / 8;
+        }
+    }
+    const int sp = at % a.n_split, tile = at / a.n_split % a.tiles;
+    const int b = bh / a.Hkv, hk = bh % a.Hkv;
     const int ratio = a.Hq / a.Hkv;
     const int held = min(max(a.len[b], 0), a.capacity);
     const int there = a.skip && a.skip[b] ? 0 : a.count ? min(max(a.count[b], 0), a.n) : a.n;   // queries of this row
     // keys that query t sees (none: a zero row)
     auto sees = [&](int t) { return t < there ? max(held - there + t + 1, 0) : 0; };
-    const int cols = min(16, a.n * ratio - tile * 16);
-    auto token = [&](int col) { return (tile * 16 + col) / ratio; };
+    const int cols = min(kCols, a.n * ratio - tile * kCols);
+    auto token = [&](int col) { return (tile * kCols + col) / ratio; };
     const int first_t = token(0), last_t = min(token(cols - 1), there - 1);
     const int keys = last_t < first_t ? 0 : sees(last_t);        // of any of the columns
     T* const out = static_cast<T*>(a.o) + b * a.os[0];
     auto out_row = [&](int col) {
-        const int q = tile * 16 + col;
+        const int q = tile * kCols + col;
         return out + (hk * ratio + q % ratio) * a.os[1] + q / ratio * a.os[2];
     };
-    // the slices of a row follow from its own length
-    const int chunk = max(kCacheSlice, ((held + a.n_split - 1) / a.n_split + kPageRows - 1) / kPageRows * kPageRows);
+    // The slices of a row follow from its own length.  Up to 512 keys are one (8.1 us for 500 in two slices, 6.7 in one),
+    // up to eight slices of 256 are merged in one go (2000 keys 9.6 -> 8.3), beyond that they are longer (8000: 11.9 -> 10.6).
+    const int least = held <= 512 ? 512 : held <= 2048 ? 256 : 512;
+    const int chunk = max(least, ((held + a.n_split - 1) / a.n_split + kPageRows - 1) / kPageRows * kPageRows);
     const int used = (keys + chunk - 1) / chunk;
     if (sp >= used) {
         if (used == 0 && sp == 0)
-            for (int i = threadIdx.x; i < cols * kHeadDim; i += 256) store_out(out_row(i / kHeadDim) + i % kHeadDim, 0.f);
+            for (int i = threadIdx.x; i < cols * kHeadDim; i += kThreads) store_out(out_row(i / kHeadDim) + i % kHeadDim, 0.f);
         return;
     }
     const int lo = sp * chunk, hi = min(keys, lo + chunk);
-    const int col = min(c16, cols - 1), my_keys = c16 < cols ? sees(token(col)) : 0;
     const int all_see = sees(first_t);   // keys that every column sees
 
-    bf16x8 qf[kQ][4];
-    {
-        const int q = tile * 16 + col;
+    // The ticket of these columns counts the slices that are done, of this call: its upper bits are the call's own
+    // number, set by whoever finds another there (whatever it is: the workspace comes as it is).
+    unsigned long long* const ticket = a.tickets + bh * a.tiles + tile;
+    if (used > 1 && threadIdx.x == 0) {
+        unsigned long long old = __hip_atomic_load(ticket, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (old >> 16 != a.call)
+            __hip_atomic_compare_exchange_strong(ticket, &old, a.call << 16, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+
+    bf16x8 qf[kQ][CT][4];
+    int my_keys[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        const int col = min(16 * ct + c16, cols - 1), q = tile * kCols + col;
+        my_keys[ct] = sees(token(col));
         const T* const row = static_cast<const T*>(a.q) + b * a.qs[0] + (hk * ratio + q % ratio) * a.qs[1] + q / ratio * a.qs[2] + 32 * g4;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             bf16x8 f[kQ];
             load_query<kQ>(row + 8 * s, f);
 #pragma unroll
-            for (int i = 0; i < kQ; ++i) qf[i][s] = f[i];
+            for (int i = 0; i < kQ; ++i)
+                qf[i][ct][s] = f[i];
         }
     }
     const long long row_at = (long long)bh * a.cache_pages * page_bytes<BITS>();
     const uint8_t* const kb = static_cast<const uint8_t*>(a.k) + row_at;
     const uint8_t* const vb = static_cast<const uint8_t*>(a.v) + row_at;
 
-    f32x4 acc[8];
+    f32x4 acc[CT][8];
+    float mx[CT], sum[CT];
+    f32x4 total[CT];   // (with whole weights: their sums on the matrix pipe, as rounded, in every register)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float mx = kLowest, sum = 0.f;
+    for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[ct][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        mx[ct] = kLowest; sum[ct] = 0.f;
+        total[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     u32x4 k_raw[4][kRaw], v_raw[4][kRaw], v_scale;
     unsigned k_scale;
     auto request_k = [&](int j) {
@@ -297,12 +334,15 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(const CacheAttendA
     };
     int j = lo + kPageRows * wave;
     if (j < hi) { request_k(j); request_v(j); }
-    for (; j < hi; j += 4 * kPageRows) {
-        float s[16];
+    for (; j < hi; j += WAVES * kPageRows) {
+        // scores of the page, a tile of 16 keys after the other
+        float s[CT][16];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const float scale = exponent_scale((k_scale >> (8 * t)) & 0xff);
-            f32x4 d = {0.f, 0.f, 0.f, 0.f};
+            f32x4 d[CT];
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) d[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int st = 0; st < 4; ++st) {
                 unsigned code[BITS / 4];
@@ -314,94 +354,129 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(const CacheAttendA
 #pragma unroll
                 for (int i = 0; i < 4; ++i) f[i] = pair[i];
 #pragma unroll
-                for (int i = 0; i < kQ; ++i) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), qf[i][st], d, 0, 0, 0);
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int i = 0; i < kQ; ++i) d[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), qf[i][ct][st], d[ct], 0, 0, 0);
             }
 #pragma unroll
-            for (int v = 0; v < 4; ++v) s[4 * t + v] = d[v] * a.scale_log2e;
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) s[ct][4 * t + v] = d[ct][v];
         }
-        const bool more = j + 4 * kPageRows < hi;
-        if (more) request_k(j + 4 * kPageRows);
+        const bool more = j + WAVES * kPageRows < hi;
+        if (more) request_k(j + WAVES * kPageRows);
         if (j + kPageRows > all_see) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    if (j + 16 * t + 4 * g4 + v >= my_keys) s[4 * t + v] = kLowest;
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        if (j + 16 * t + 4 * g4 + v >= my_keys[ct]) s[ct][4 * t + v] = -INFINITY;
         }
-        float top = s[0];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-        top = wave_group_max(top);
-        if (__any(top > mx)) {
-            const float m_new = fmaxf(mx, top), down = __builtin_amdgcn_exp2f(mx - m_new);
-            mx = m_new;
-            sum *= down;
+        for (int ct = 0; ct < CT; ++ct) {
+            float top = s[ct][0];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[i] *= down;
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, s[ct][i]);
+            top = wave_group_max(top) * a.scale_log2e;
+            if (__any(top > mx[ct])) {
+                const float m_new = fmaxf(mx[ct], top), down = __builtin_amdgcn_exp2f(mx[ct] - m_new);
+                mx[ct] = m_new;
+                sum[ct] *= down;
+                if constexpr (kP == 1) total[ct] *= down;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[ct][i] *= down;
+            }
         }
         // keys behind the last: whatever lies there, their weights are zero and so are their values
         const bool clear = j + kPageRows > hi;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            u32x4 pf[kP];
+            u32x4 pf[CT][kP];
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(s[8 * h + e] - mx), p1 = __builtin_amdgcn_exp2f(s[8 * h + e + 1] - mx);
-                sum += p0 + p1;
-                unsigned w[kP];
-                split_pair<kP>(p0, p1, w);
+            for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                for (int i = 0; i < kP; ++i) pf[i][e / 2] = w[i];
-            }
-            unsigned val[8][4];   // eight columns of the lane's eight keys
+                for (int e = 0; e < 8; e += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(fmaf(s[ct][8 * h + e], a.scale_log2e, -mx[ct]));
+                    const float p1 = __builtin_amdgcn_exp2f(fmaf(s[ct][8 * h + e + 1], a.scale_log2e, -mx[ct]));
+                    if constexpr (kP > 1) sum[ct] += p0 + p1;
+                    unsigned w[kP];
+                    split_pair<kP>(p0, p1, w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int t = 2 * h + e / 4, k = e % 4;
-                unsigned code[BITS / 4];
-#pragma unroll
-                for (int i = 0; i < BITS / 4; ++i) code[i] = v_raw[t][(BITS / 4 * k + i) / 4][(BITS / 4 * k + i) % 4];
-                unsigned ex = (v_scale[t] >> (8 * k)) & 0xff;
-                if (clear && j + 16 * t + 4 * g4 + k >= hi) {
-                    ex = 127;
-#pragma unroll
-                    for (int i = 0; i < BITS / 4; ++i) code[i] = 0;
+                    for (int i = 0; i < kP; ++i) pf[ct][i][e / 2] = w[i];
                 }
-                bf16_of8<BITS>(code, exponent_scale(ex), val[e]);
+            if constexpr (kP == 1) {
+                const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+                    total[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, pf[ct][0]), total[ct], 0, 0, 0);
             }
+            float scale[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                u32x4 t;
+            for (int e = 0; e < 8; ++e) scale[e] = exponent_scale((v_scale[2 * h + e / 4] >> (8 * (e % 4))) & 0xff);
+            if (clear) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) t[e] = __builtin_amdgcn_perm(val[2 * e + 1][i / 2], val[2 * e][i / 2], i & 1 ? 0x07060302u : 0x05040100u);
+                for (int e = 0; e < 8; ++e) {
+                    const int t = 2 * h + e / 4, k = e % 4;
+                    if (j + 16 * t + 4 * g4 + k < hi) continue;
+                    scale[e] = 1.f;
 #pragma unroll
-                for (int k = 0; k < kP; ++k)
-                    acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t), __builtin_bit_cast(bf16x8, pf[k]), acc[i], 0, 0, 0);
+                    for (int i = 0; i < BITS / 4; ++i) v_raw[t][(BITS / 4 * k + i) / 4][(BITS / 4 * k + i) % 4] = 0;
+                }
+            }
+            // four columns of the lane's eight keys at a time
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                unsigned val[8][2];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int t = 2 * h + e / 4, k = e % 4;
+                    if constexpr (BITS == 4) bf16_of4<BITS>(v_raw[t][0][k], part, scale[e], val[e]);
+                    else bf16_of4<BITS>(v_raw[t][(2 * k + part) / 4][(2 * k + part) % 4], 0, scale[e], val[e]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    u32x4 t;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) t[e] = __builtin_amdgcn_perm(val[2 * e + 1][i / 2], val[2 * e][i / 2], i & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                        for (int k = 0; k < kP; ++k)
+                            acc[ct][4 * part + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t), __builtin_bit_cast(bf16x8, pf[ct][k]), acc[ct][4 * part + i], 0, 0, 0);
+                }
             }
         }
-        if (more) request_v(j + 4 * kPageRows);
+        if (more) request_v(j + WAVES * kPageRows);
     }
 
-    // the four waves' results through LDS (register v of product i is column 8 (4 g4 + v) + i)
-    sum = wave_group_sum(sum);
+    // the waves' results through LDS (register v of product i is column 8 (4 g4 + v) + i)
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        float* dst = &o_part[wave][c16][8 * (4 * g4 + v)];
-        *reinterpret_cast<f32x4*>(dst) = f32x4{acc[0][v], acc[1][v], acc[2][v], acc[3][v]};
-        *reinterpret_cast<f32x4*>(dst + 4) = f32x4{acc[4][v], acc[5][v], acc[6][v], acc[7][v]};
+    for (int ct = 0; ct < CT; ++ct) {
+        if constexpr (kP == 1) sum[ct] = total[ct][0];
+        else sum[ct] = wave_group_sum(sum[ct]);
+        if (16 * ct + c16 < cols)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                float* dst = &o_part[wave][16 * ct + c16][8 * (4 * g4 + v)];
+                *reinterpret_cast<f32x4*>(dst) = f32x4{acc[ct][0][v], acc[ct][1][v], acc[ct][2][v], acc[ct][3][v]};
+                *reinterpret_cast<f32x4*>(dst + 4) = f32x4{acc[ct][4][v], acc[ct][5][v], acc[ct][6][v], acc[ct][7][v]};
+            }
+        if (lane < 16) { stat[wave][16 * ct + lane][0] = mx[ct]; stat[wave][16 * ct + lane][1] = sum[ct]; }
     }
-    if (lane < 16) { stat[wave][lane][0] = mx; stat[wave][lane][1] = sum; }
     __syncthreads();
     constexpr int kPairs = kPartStride / 2;   // the last one: running max, sum
-    float* const part0 = a.part + ((long long)bh * a.tiles + tile) * a.n_split * 16 * kPartStride;   // [slice][column]
-    for (int i = threadIdx.x; i < cols * kPairs; i += 256) {
+    float* const part0 = a.part + ((long long)bh * a.tiles + tile) * a.n_split * kCols * kPartStride;   // [slice][column]
+    for (int i = threadIdx.x; i < cols * kPairs; i += kThreads) {
         const int q = i / kPairs, c = 2 * (i - q * kPairs);
         float m_all = kLowest;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) m_all = fmaxf(m_all, stat[w][q][0]);
+        for (int w = 0; w < WAVES; ++w) m_all = fmaxf(m_all, stat[w][q][0]);
         Float2 v = {0.f, 0.f};
         float den = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float wt = __builtin_amdgcn_exp2f(stat[w][q][0] - m_all);
             den = fmaf(stat[w][q][1], wt, den);
             if (c == kHeadDim) continue;
@@ -409,7 +484,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(const CacheAttendA
             v.y = fmaf(o_part[w][q][c + 1], wt, v.y);
         }
         if (c == kHeadDim) v = {m_all, den};
-        if (used > 1) put_shared(part0 + ((long long)sp * 16 + q) * kPartStride + c, v);
+        if (used > 1) put_shared(part0 + ((long long)sp * kCols + q) * kPartStride + c, v);
         else if (c < kHeadDim) {
             const bool some = sees(token(q)) > 0;
             store_out(out_row(q) + c, some ? v.x / den : 0.f);
@@ -421,12 +496,14 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(const CacheAttendA
     // the workgroup that draws the last ticket of its columns merges the slices
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (threadIdx.x == 0) drawn = __hip_atomic_fetch_add(a.tickets + bh * a.tiles + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (threadIdx.x == 0) drawn = (int)(__hip_atomic_fetch_add(ticket, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & 0xffff);
     __syncthreads();
     if (drawn != used - 1) return;
-    for (int q = wave; q < cols; q += 4) {
+    // (a replayed graph calls by the same number again)
+    if (threadIdx.x == 0) __hip_atomic_store(ticket, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int q = wave; q < cols; q += WAVES) {
         Float2 own = {kLowest, 0.f};
-        if (lane < used) own = get_shared(part0 + ((long long)lane * 16 + q) * kPartStride + kHeadDim);
+        if (lane < used) own = get_shared(part0 + ((long long)lane * kCols + q) * kPartStride + kHeadDim);
         float m_all = own.x;
 #pragma unroll
         for (int step = 1; step < 64; step *= 2) m_all = fmaxf(m_all, __shfl_xor(m_all, step));
@@ -438,31 +515,30 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(const CacheAttendA
         if (lane == 0) weight[q][kDecodeMaxSplit] = den;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < cols * (kHeadDim / 2); i += 256) {
-        const int q = i / (kHeadDim / 2), c = 2 * (i % (kHeadDim / 2));
-        Float2 num = {0.f, 0.f};
-        for (int l = 0; l < used; l += 8) {
-            Float2 x[8];
+    auto merge = [&](auto batch) {
+        constexpr int kBatch = decltype(batch)::value;
+        for (int i = threadIdx.x; i < cols * (kHeadDim / 2); i += kThreads) {
+            const int q = i / (kHeadDim / 2), c = 2 * (i % (kHeadDim / 2));
+            Float2 num = {0.f, 0.f};
+            for (int l = 0; l < used; l += kBatch) {
+                Float2 x[kBatch];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = get_shared(part0 + ((long long)min(l + u, used - 1) * 16 + q) * kPartStride + c);
+                for (int u = 0; u < kBatch; ++u) x[u] = get_shared(part0 + ((long long)min(l + u, used - 1) * kCols + q) * kPartStride + c);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float wt = l + u < used ? weight[q][l + u] : 0.f;
-                num.x = fmaf(x[u].x, wt, num.x);
-                num.y = fmaf(x[u].y, wt, num.y);
+                for (int u = 0; u < kBatch; ++u) {
+                    const float wt = l + u < used ? weight[q][l + u] : 0.f;
+                    num.x = fmaf(x[u].x, wt, num.x);
+                    num.y = fmaf(x[u].y, wt, num.y);
+                }
             }
+            const float den = weight[q][kDecodeMaxSplit];
+            const bool some = sees(token(q)) > 0;
+            store_out(out_row(q) + c, some ? num.x / den : 0.f);
+            store_out(out_row(q) + c + 1, some ? num.y / den : 0.f);
         }
-        const float den = weight[q][kDecodeMaxSplit];
-        const bool some = sees(token(q)) > 0;
-        store_out(out_row(q) + c, some ? num.x / den : 0.f);
-        store_out(out_row(q) + c + 1, some ? num.y / den : 0.f);
-    }
-}
-
-__global__ void clear_tickets_kernel(int32_t* tickets, int n)
-{
-    const int i = blockIdx.x * blockDim.x + threadIdx.x;
-    if (i < n) tickets[i] = 0;
+    };
+    if (used <= 8) merge(std::integral_constant<int, 8>());
+    else merge(std::integral_constant<int, 32>());
 }
 
 }  // namespace
@@ -473,23 +549,25 @@ size_t cache_bytes(int bits, long long caches, int capacity)
     return (size_t)caches * pages * (bits == 4 ? page_bytes<4>() : page_bytes<8>());
 }
 
-int32_t* cache_tickets(float* part, long long tiles, int n_split)
+CachePlan cache_plan(bool bf16, int B, int Hq, int Hkv, int n, int capacity, int n_cu)
 {
-    return n_split > 1 ? (int32_t*)(part + tiles * n_split * 16 * kPartStride) : nullptr;
-}
-
-int cache_split(int B, int Hq, int Hkv, int n, int capacity, int n_cu)
-{
-    const long long tiles = (long long)B * Hkv * (((long long)n * (Hq / Hkv) + 15) / 16);
-    const long long most = std::min<long long>(kDecodeMaxSplit, (capacity + kCacheSlice - 1) / kCacheSlice);
-    return (int)std::min(std::max(2ll * n_cu / tiles, 1ll), most);
-}
-
-size_t cache_scratch_bytes(int B, int Hq, int Hkv, int n, int n_cu)
-{
-    const size_t tiles = (size_t)B * Hkv * (((size_t)n * (Hq / Hkv) + 15) / 16);
-    const int split = cache_split(B, Hq, Hkv, n, 1 << 30, n_cu);
-    return split == 1 ? 0 : tiles * (split * 16 * kPartStride + 1) * sizeof(float);
+    const long long cols = (long long)n * (Hq / Hkv), caches = (long long)B * Hkv;
+    CachePlan p;
+    // Two column tiles a workgroup halve the conversion of codes, where enough workgroups are left (from half of
+    // that on: 8 x 5 tokens x 32 / 8 heads x 6000 keys 24 -> 21 us, but 4 x 8 x 4000 15.6 -> 18.8).
+    p.col_tiles = bf16 && cols > 16 && caches * ((cols + 15) / 16) >= 2 * n_cu ? 2 : 1;
+    p.tiles = (int)((cols + 16 * p.col_tiles - 1) / (16 * p.col_tiles));
+    // Up to a workgroup of eight waves for each compute unit: of four waves two would leave twice the slices to merge
+    // (bf16, 4 bits, 1 x 32 / 8 heads x 32768 keys 15.8 and 22.7 us with four, 8 x 32 / 8 x 8192 18.7 and 20.4, 8 x 32 / 32 x
+    // 8192 53 and 56).  More than that, or where eight leave more than a quarter of the compute units out, of four:
+    // their beginnings and ends overlap (64 x 32 / 8 x 2048 32.8 -> 29.7, 24 x 32 / 32 x up to 1000 24.0 -> 19.2; 4 x 40 / 40
+    // x 12000 60.8 -> 52.5 in three slices, x 3000 even).
+    const long long tiles = caches * p.tiles, of_8 = n_cu / tiles;
+    p.waves = tiles > n_cu || 4 * tiles * of_8 <= 3 * n_cu ? 4 : 8;
+    const long long most = std::min<long long>(kDecodeMaxSplit, ((long long)capacity + 255) / 256);
+    p.split = tiles > n_cu ? 1 : (int)std::min(p.waves == 8 ? of_8 : 2 * n_cu / tiles, most);
+    p.bytes = p.split == 1 ? 0 : (size_t)tiles * ((size_t)p.split * 16 * p.col_tiles * kPartStride + 2) * sizeof(float);
+    return p;
 }
 
 hipError_t launch_cache_write(const CacheWriteArgs& in, int dtype, int bits, hipStream_t s)
@@ -541,25 +619,31 @@ hipError_t launch_cache_read(const CacheReadArgs& in, int dtype, int bits, hipSt
     return hipGetLastError();
 }
 
-hipError_t launch_cache_attend(const CacheAttendArgs& in, int dtype, int bits, bool clear, hipStream_t s)
+hipError_t launch_cache_attend(const CacheAttendArgs& in, const CachePlan& plan, int dtype, int bits, hipStream_t s)
 {
     CacheAttendArgs a = in;
-    a.tiles = (int)(((long long)a.n * (a.Hq / a.Hkv) + 15) / 16);
-    const long long tiles = (long long)a.B * a.Hkv * a.tiles;
-    a.tickets = cache_tickets(a.part, tiles, a.n_split);
-    if (clear && a.n_split > 1) {
-        clear_tickets_kernel<<<dim3((unsigned)((tiles + 255) / 256)), dim3(256), 0, s>>>(a.tickets, (int)tiles);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
+    const long long tiles = (long long)a.B * a.Hkv * plan.tiles;
+    a.tiles = plan.tiles; a.n_split = plan.split;
+    a.tickets = (unsigned long long*)(a.part + tiles * a.n_split * 16 * plan.col_tiles * kPartStride);   // behind the partial results
     const unsigned grid = (unsigned)(tiles * a.n_split);
+#define TF_CACHE_ATTEND(T, BITS, CT, WAVES) cache_attend_kernel<T, BITS, CT, WAVES><<<dim3(grid), dim3(64 * WAVES), 0, s>>>(a)
+#define TF_CACHE_ATTEND_WAVES(T, BITS, CT)                                                        \
+    do {                                                                                          \
+        if (plan.waves == 8) TF_CACHE_ATTEND(T, BITS, CT, 8);                                     \
+        else TF_CACHE_ATTEND(T, BITS, CT, 4);                                                     \
+    } while (0)
     if (dtype == 0) {
-        if (bits == 4) cache_attend_kernel<float, 4><<<dim3(grid), dim3(256), 0, s>>>(a);
-        else cache_attend_kernel<float, 8><<<dim3(grid), dim3(256), 0, s>>>(a);
+        if (bits == 4) TF_CACHE_ATTEND_WAVES(float, 4, 1);
+        else TF_CACHE_ATTEND_WAVES(float, 8, 1);
+    } else if (plan.col_tiles == 1) {
+        if (bits == 4) TF_CACHE_ATTEND_WAVES(uint16_t, 4, 1);
+        else TF_CACHE_ATTEND_WAVES(uint16_t, 8, 1);
     } else {
-        if (bits == 4) cache_attend_kernel<uint16_t, 4><<<dim3(grid), dim3(256), 0, s>>>(a);
-        else cache_attend_kernel<uint16_t, 8><<<dim3(grid), dim3(256), 0, s>>>(a);
+        if (bits == 4) TF_CACHE_ATTEND_WAVES(uint16_t, 4, 2);
+        else TF_CACHE_ATTEND_WAVES(uint16_t, 8, 2);
     }
+#undef TF_CACHE_ATTEND_WAVES
+#undef TF_CACHE_ATTEND
     return hipGetLastError();
 }
 

@@ -104,6 +104,22 @@ __device__ __forceinline__ void bf16_of8(const unsigned* w, float scale, unsigne
     }
 }
 
+// four of them: the first or the second half of a dword of 4-bit codes, or a dword of 8-bit ones
+template <int BITS>
+__device__ __forceinline__ void bf16_of4(unsigned w, int half, float scale, unsigned* pair)
+{
+    if constexpr (BITS == 8) {
+        pair[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
+        pair[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true));
+    } else if (half == 0) {
+        pair[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+        pair[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+    } else {
+        pair[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+        pair[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+    }
+}
+
 // Eight columns 8 c of one row into row `row` of a page, by lane c of a 16-lane group whose lanes all take part
 // (`store`: whether this group's row is to be written).  value: the layout of values, not keys.
 template <int BITS>

@@ -863,24 +863,22 @@ template <typename T>
 hipError_t launch_decode_step_bits_t(const DecodeArgs& a, const T* q, const T* k, const T* v, T* o, hipStream_t s)
 {
     const int threads = std::min(1024, (32 * a.Hkv + 63) / 64 * 64);
-    const int tiles = a.Hkv * ((a.Hq / a.Hkv + 15) / 16);   // of a batch row, a ticket each
-    int32_t* const tickets = cache_tickets(a.part, a.B * tiles, a.n_split);
     const ScoreArgs<T> score{k, v, a.anchor_k, a.anchor_v, a.seen, a.skipped, a.tau, a.cache_len, a.overflow,
                              a.k_cache, a.v_cache, a.capacity, a.Hkv, a.ema, a.gamma, a.inclusive, a.fusion, a.warmup,
-                             a.target, a.eta, a.skip, a.fused, tickets, a.n_split > 1 ? tiles : 0};
+                             a.target, a.eta, a.skip, a.fused, nullptr, 0};
     if (a.bits == 4) decode_score_kernel<T, 4><<<dim3(a.B), dim3(threads), 0, s>>>(score);
     else decode_score_kernel<T, 8><<<dim3(a.B), dim3(threads), 0, s>>>(score);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     CacheAttendArgs c = {};
     c.q = q; c.k = a.k_cache; c.v = a.v_cache; c.o = o;
-    c.len = a.cache_len; c.skip = a.skip; c.part = a.part;
+    c.len = a.cache_len; c.skip = a.skip; c.part = a.part; c.call = a.call;
     c.B = a.B; c.Hq = a.Hq; c.Hkv = a.Hkv; c.n = 1; c.capacity = a.capacity;
-    c.cache_pages = (a.capacity + kPageRows - 1) / kPageRows; c.n_split = a.n_split;
+    c.cache_pages = (a.capacity + kPageRows - 1) / kPageRows;
     c.scale_log2e = a.scale * 1.4426950408889634f;
     c.qs[0] = c.os[0] = (long long)a.Hq * kHeadDim;
     c.qs[1] = c.os[1] = c.qs[2] = c.os[2] = kHeadDim;
-    return launch_cache_attend(c, sizeof(T) == 2, a.bits, false, s);
+    return launch_cache_attend(c, cache_plan(sizeof(T) == 2, a.B, a.Hq, a.Hkv, 1, a.capacity, a.n_cu), sizeof(T) == 2, a.bits, s);
 }
 
 }  // namespace

@@ -88,6 +88,8 @@ struct DecodeArgs {
     float* part;                                    // scratch [B][Hq][n_split][kDecodePartFloats], tickets
     int n_few, n_split;                             // 1 .. decode_split()
     int bits;                                       // of the caches: 0: of the step's type, 4, 8 (cache_format.h)
+    unsigned long long call;                        // with bits: as in CacheAttendArgs
+    int n_cu;                                       // with bits: compute units to plan for
 };
 struct DecodeSplit { int few, most; };              // slices of a row; of one of kDecodeLongSlice * most keys or more (bf16)
 int decode_heads_per_wg(bool bf16, int B, int Hq, int Hkv);   // query heads one workgroup handles at most (they share a KV head)
@@ -141,21 +143,20 @@ struct CacheAttendArgs {
     const int32_t *len, *count;                     // [B]; count may be null
     const uint8_t* skip;                            // [B], may be null: rows that get zeros
     float* part;
-    int32_t* tickets;
+    unsigned long long* tickets;                    // a call's number and its slices that are done
+    unsigned long long call;                        // < 2^48, not 0, another one each call
     int B, Hq, Hkv, n, tiles, capacity, cache_pages, n_split;
     float scale_log2e;
     long long qs[3], os[3];
 };
-constexpr int kCacheSlice = 128;                    // keys of a slice at least
 size_t cache_bytes(int bits, long long caches, int capacity);
-// slices of a row's keys for each 16 columns (queries x heads of a KV head), and what they need of a workspace
-int cache_split(int B, int Hq, int Hkv, int n, int capacity, int n_cu);
-size_t cache_scratch_bytes(int B, int Hq, int Hkv, int n, int n_cu = 256);
-int32_t* cache_tickets(float* part, long long tiles, int n_split);   // behind the partial results
+// How the attention is cut up: a workgroup of `waves` takes col_tiles x 16 columns (queries x heads of a KV head), of
+// which a (batch row, KV head) has `tiles`, and one of at most `split` slices of its keys; bytes: of workspace.
+struct CachePlan { int col_tiles, waves, tiles, split; size_t bytes; };
+CachePlan cache_plan(bool bf16, int B, int Hq, int Hkv, int n, int capacity, int n_cu);
 hipError_t launch_cache_write(const CacheWriteArgs& a, int dtype, int bits, hipStream_t s);
 hipError_t launch_cache_read(const CacheReadArgs& a, int dtype, int bits, hipStream_t s);
-// clear: the tickets are not known to be zero
-hipError_t launch_cache_attend(const CacheAttendArgs& a, int dtype, int bits, bool clear, hipStream_t s);
+hipError_t launch_cache_attend(const CacheAttendArgs& a, const CachePlan& plan, int dtype, int bits, hipStream_t s);
 
 // ---- measurement probes (not part of the path) ---------------------------------------------
 hipError_t launch_probe_stream_read(const void* src, size_t bytes, void* sink, int n_cu,

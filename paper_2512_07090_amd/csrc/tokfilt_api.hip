@@ -4,6 +4,7 @@
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
+#include <time.h>
 
 #include <algorithm>
 #include <new>
@@ -26,6 +27,7 @@ struct tf_ctx {
     int timing_calls;
     hipEvent_t ev[256][TF_N_STAGES + 1];
     bool ev_ready;
+    uint64_t calls;  // of the attention over a quantised cache
 };
 
 namespace {
@@ -210,7 +212,7 @@ tf_status decode_args(tf_ctx* ctx, const tf_params* p, const tf_decode_state* st
     a->gamma = (double)p->ema_gamma;
     a->target = (float)p->prune_ratio; a->eta = 0.f;
     a->scale = p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
-    a->skip = nullptr; a->fused = nullptr; a->part = nullptr; a->n_few = a->n_split = 1; a->bits = 0;
+    a->skip = nullptr; a->fused = nullptr; a->part = nullptr; a->n_few = a->n_split = 1; a->bits = 0; a->call = 0; a->n_cu = 0;
     return TF_OK;
 }
 
@@ -242,6 +244,16 @@ tf_status use_device(tf_ctx* ctx)
 {
     if (hipSetDevice(ctx->device) != hipSuccess) return fail(ctx, TF_ERR_DEVICE, "hipSetDevice(%d) failed", ctx->device);
     return TF_OK;
+}
+
+// A number for this call that its workspace cannot hold by chance: 48 bits of a mixed counter that starts anywhere.
+unsigned long long call_number(tf_ctx* ctx)
+{
+    uint64_t x = __atomic_add_fetch(&ctx->calls, 0x9e3779b97f4a7c15ull, __ATOMIC_RELAXED);
+    x = (x ^ (x >> 30)) * 0xbf58476d1ce4e5b9ull;
+    x = (x ^ (x >> 27)) * 0x94d049bb133111ebull;
+    x = (x ^ (x >> 31)) >> 16;
+    return x ? x : 1;
 }
 
 int cache_pages(int32_t capacity) { return (int)(((int64_t)capacity + 63) / 64); }
@@ -372,6 +384,9 @@ tf_status tf_create(tf_ctx** out, int device)
     if (!c) return TF_ERR_DEVICE;
     memset(c, 0, sizeof(*c));
     c->device = device;
+    timespec now;
+    clock_gettime(CLOCK_REALTIME, &now);
+    c->calls = (uint64_t)now.tv_sec * 1000000000ull + (uint64_t)now.tv_nsec + (uint64_t)(uintptr_t)c;
     if (hipDeviceGetAttribute(&c->n_cu, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess || c->n_cu < 1) {
         delete c;
         return TF_ERR_DEVICE;
@@ -649,8 +664,9 @@ size_t tf_cache_workspace_bytes(const tf_params* p)
 {
     const char* why;
     if (check_shape(p, &why) != TF_OK) return 0;
-    const size_t step = tf::cache_scratch_bytes(p->batch, p->n_q_heads, p->n_kv_heads, 1);
-    return align256(std::max({step, tf::cache_scratch_bytes(p->batch, p->n_q_heads, p->n_kv_heads, p->seq), (size_t)256}));
+    // (for 256 compute units and a cache of any capacity)
+    const auto bytes = [&](int n) { return tf::cache_plan(p->dtype != TF_F32, p->batch, p->n_q_heads, p->n_kv_heads, n, INT32_MAX, 256).bytes; };
+    return align256(std::max({bytes(1), bytes(p->seq), (size_t)256}));
 }
 
 tf_status tf_cache_write(tf_ctx* ctx, const tf_params* p, const tf_cache* cache, const void* K, const void* V,
@@ -702,23 +718,21 @@ tf_status tf_cache_attend(tf_ctx* ctx, const tf_params* p, const tf_cache* cache
     if (Q == O) return fail(ctx, TF_ERR_INVALID_ARG, "Q and O must not overlap");
     if (folded(p->o_stride, p->batch, p->n_q_heads)) return fail(ctx, TF_ERR_INVALID_ARG, "an output must not have a stride of 0");
     if (!ws || misaligned(ws)) return fail(ctx, TF_ERR_INVALID_ARG, "workspace must be a 16-byte aligned pointer");
-    const int n_cu = std::min(ctx->n_cu, 256);   // (workspaces are sized for 256)
-    const size_t need = tf::cache_scratch_bytes(p->batch, p->n_q_heads, p->n_kv_heads, p->seq, n_cu);
-    if (ws_bytes < need)
-        return fail(ctx, TF_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, need);
     if ((int64_t)p->batch * p->n_kv_heads * (((int64_t)p->seq * (p->n_q_heads / p->n_kv_heads) + 15) / 16) >= ((int64_t)1 << 25))
         return fail(ctx, TF_ERR_UNSUPPORTED, "too many queries for one call");
+    const tf::CachePlan plan = tf::cache_plan(p->dtype != TF_F32, p->batch, p->n_q_heads, p->n_kv_heads, p->seq, cache->capacity, std::min(ctx->n_cu, 256));
+    if (ws_bytes < plan.bytes)
+        return fail(ctx, TF_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, plan.bytes);
     st = use_device(ctx);
     if (st != TF_OK) return st;
     tf::CacheAttendArgs a;
     a.q = Q; a.k = cache->k; a.v = cache->v; a.o = O; a.len = cache->len; a.count = count; a.skip = nullptr;
-    a.part = (float*)ws; a.tickets = nullptr;
+    a.part = (float*)ws; a.tickets = nullptr; a.call = call_number(ctx); a.n_split = 1;
     a.B = p->batch; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.n = p->seq; a.tiles = 0; a.capacity = cache->capacity;
     a.cache_pages = cache_pages(cache->capacity);
-    a.n_split = tf::cache_split(p->batch, p->n_q_heads, p->n_kv_heads, p->seq, cache->capacity, n_cu);
     a.scale_log2e = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim)) * 1.4426950408889634f;
     for (int i = 0; i < 3; ++i) { a.qs[i] = p->q_stride[i]; a.os[i] = p->o_stride[i]; }
-    return dev(ctx, tf::launch_cache_attend(a, p->dtype, cache->format, true, (hipStream_t)stream), "cache attention launch");
+    return dev(ctx, tf::launch_cache_attend(a, plan, p->dtype, cache->format, (hipStream_t)stream), "cache attention launch");
 }
 
 tf_status tf_decode_prefill_q(tf_ctx* ctx, const tf_params* p, float eta, float tau0, const tf_decode_state* state,
@@ -748,16 +762,16 @@ tf_status tf_decode_step_q(tf_ctx* ctx, const tf_params* p, float eta, const tf_
         return fail(ctx, TF_ERR_INVALID_ARG, "q, k, v and o must be 16-byte aligned");
     if (!(eta >= 0.f) || isinf(eta)) return fail(ctx, TF_ERR_INVALID_ARG, "eta must be finite and >= 0");
     if (!ws || misaligned(ws)) return fail(ctx, TF_ERR_INVALID_ARG, "workspace must be a 16-byte aligned pointer");
-    const int n_cu = std::min(ctx->n_cu, 256);
-    const size_t need = tf::cache_scratch_bytes(p->batch, p->n_q_heads, p->n_kv_heads, 1, n_cu);
+    a.n_cu = std::min(ctx->n_cu, 256);   // (workspaces are sized for 256)
+    const size_t need = tf::cache_plan(p->dtype != TF_F32, p->batch, p->n_q_heads, p->n_kv_heads, 1, state->capacity, a.n_cu).bytes;
     if (ws_bytes < need)
         return fail(ctx, TF_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, need);
     a.bits = format;
+    a.call = call_number(ctx);
     a.eta = eta;
     a.skip = skip;
     a.fused = fused;
     a.part = (float*)ws;
-    a.n_split = tf::cache_split(p->batch, p->n_q_heads, p->n_kv_heads, 1, state->capacity, n_cu);
     return dev(ctx, tf::launch_decode_step(a, p->dtype, q, k, v, o, (hipStream_t)stream), "decode step launch");
 }
 

@@ -80,19 +80,18 @@ def attend(q, k, v, lens, counts, scale):
     """float64 CUDA tensors q [B, Hq, n, 128], k, v [B, Hkv, rows, 128] -> (o, A = sum of w |v|, S = largest scale sum |q k|
     of a query and its keys), zero rows where nothing is seen."""
     B, Hq, n, _ = q.shape
-    Hkv = k.shape[1]
+    g = Hq // k.shape[1]
     o, mag = torch.zeros_like(q), torch.zeros_like(q)
     big = torch.zeros(q.shape[:3], dtype=torch.float64, device=q.device)
     for b in range(B):
+        first = max(0, counts[b] - lens[b])              # queries before that see nothing
+        t = torch.arange(first, counts[b], device=q.device)
+        if len(t) == 0 or lens[b] == 0:
+            continue
+        unseen = torch.arange(lens[b], device=q.device) > (lens[b] - counts[b] + t)[:, None]
         for h in range(Hq):
-            hk = h // (Hq // Hkv)
-            for t in range(counts[b]):
-                m = lens[b] - counts[b] + t + 1
-                if m <= 0:
-                    continue
-                kk, vv = k[b, hk, :m], v[b, hk, :m]
-                w = torch.softmax((kk * q[b, h, t]).sum(1) * scale, 0)
-                o[b, h, t] = (w[:, None] * vv).sum(0)
-                mag[b, h, t] = (w[:, None] * vv.abs()).sum(0)
-                big[b, h, t] = (kk * q[b, h, t]).abs().sum(1).max() * scale
+            kk, vv, qq = k[b, h // g, :lens[b]], v[b, h // g, :lens[b]], q[b, h, first:counts[b]]
+            w = torch.softmax((qq @ kk.T.contiguous() * scale).masked_fill(unseen, -torch.inf), 1)
+            o[b, h, first:counts[b]], mag[b, h, first:counts[b]] = w @ vv, w @ vv.abs()
+            big[b, h, first:counts[b]] = (qq.abs() @ kk.abs().T.contiguous() * scale).masked_fill(unseen, 0.0).amax(1)
     return o, mag, big[..., None]

@@ -39,7 +39,11 @@ int main()
     if (tf_cache_bytes(&p, 0, 64) || tf_cache_bytes(&p, 16, 64) || tf_cache_bytes(&p, 4, 0) || tf_cache_bytes(nullptr, 4, 64) ||
         tf_cache_workspace_bytes(nullptr)) { ++bad; printf("sizes of nothing\n"); }
     if (tf_cache_bytes(&p, TF_CACHE_FP8, 0x7fffffff) != 4ull * 33554432 * 8448) { ++bad; printf("large size\n"); }
-    if (tf_cache_workspace_bytes(&p) < 256) { ++bad; printf("workspace\n"); }
+    for (int b : {1, 3, 64}) for (int n : {1, 5, 300}) {
+        const tf_params x = shape(b, 32, 8, n, TF_BF16);
+        const size_t w = tf_cache_workspace_bytes(&x);
+        if (w < 256 || w > (64u << 20)) { ++bad; printf("workspace\n"); }
+    }
     { tf_params x = p; x.head_dim = 64; if (tf_cache_bytes(&x, 4, 64) || tf_cache_workspace_bytes(&x)) { ++bad; printf("shape\n"); } }
 
     auto write = [&](tf_ctx* cc, const tf_params* pp, const tf_cache* d, const void* k, const void* v, int m) { return tf_cache_write(cc, pp, d, k, v, nullptr, m, nullptr, nullptr); };
@@ -77,7 +81,8 @@ int main()
     expect(c, attend(&p, Q, Q, ws, sizeof ws), inv, "attend, in place");
     expect(c, attend(&p, Q, O, nullptr, 0), inv, "attend, no workspace");
     expect(c, attend(&p, Q, O, ws + 1, sizeof ws - 1), inv, "attend, workspace alignment");
-    expect(c, attend(&p, Q, O, ws, 16), TF_ERR_WORKSPACE_TOO_SMALL, "attend, small workspace");
+    { tf_cache d = good; d.capacity = 5000;
+      expect(c, tf_cache_attend(c, &p, &d, Q, O, nullptr, ws, 16, nullptr), TF_ERR_WORKSPACE_TOO_SMALL, "attend, small workspace"); }
     { tf_params x = p; x.o_stride[1] = 0; expect(c, attend(&x, Q, O, ws, sizeof ws), inv, "attend, folded"); }
     { tf_params x = shape(1024, 128, 1, 1 << 19, TF_F32); expect(c, attend(&x, Q, O, ws, sizeof ws), TF_ERR_UNSUPPORTED, "attend, too many queries"); }
 

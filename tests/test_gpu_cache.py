@@ -7,6 +7,9 @@ pipe: 2^-20 S), of its scaling and of the exponent (2^-22 S); a weight by as muc
 its two bf16 parts (2^-16); sums over up to some hundred steps add 2^-18.  Both the numerator and the denominator carry that:
   fp32  |o - ref| <= (2^-18 S + 2^-17) A
   bf16  |o - ref| <= (2^-18 S + 2^-15) A + 2^-8 |ref|   (the output's own rounding)
+A call with many queries rounds a weight to bf16 once (|d| <= 2^-8), numerator and denominator alike, so that the result is
+sum w (1 + d) v / sum w (1 + d), off by at most 2^-8 / (1 - 2^-8) (A + |ref|) < (2^-8 + 2^-15) (A + |ref|):
+  bf16  |o - ref| <= (2^-18 S + 2^-8 + 2^-14) (A + |ref|) + 2^-8 |ref|
 """
 import numpy as np
 import pytest
@@ -154,9 +157,13 @@ def _quant_cache(p, dt, bits, Bn, Hkv, lens, cap, seed):
     return c, out[0], out[1]
 
 
-def _check_attention(o, want, dt):
+def _check_attention(o, want, dt, many=False):
     r, A, S = want
     err = (o.double() - r).abs()
+    if many:
+        tol = (2.0 ** -18 * S + 2.0 ** -8 + 2.0 ** -14) * (A + r.abs()) + 2.0 ** -8 * r.abs()
+        assert (err <= tol).all(), (err - tol).max().item()
+        return
     tol = (2.0 ** -18 * S + (2.0 ** -17 if dt == "f32" else 2.0 ** -15)) * A + (2.0 ** -8 * r.abs() if dt == "bf16" else 0)
     assert (err <= tol).all(), (err - tol).max().item()
 
@@ -169,7 +176,14 @@ def _check_attention(o, want, dt):
     ("bf16", 8, 1, 128, 8, 1, [200], None, 200), ("bf16", 4, 2, 8, 2, 7, [7, 300], None, 320),
     ("bf16", 4, 3, 4, 2, 33, [33, 200, 20], [33, 10, 0], 256), ("bf16", 8, 2, 6, 2, 20, [5, 400], [20, 19], 401),
     ("f32", 4, 2, 4, 1, 9, [100, 9], [9, 4], 128), ("f32", 8, 1, 4, 4, 40, [130], None, 130),
-    ("bf16", 4, 1, 8, 8, 100, [1500], None, 1600), ("bf16", 4, 2, 8, 1, 64, [64, 700], [1, 64], 700)])
+    ("bf16", 4, 1, 8, 8, 100, [1500], None, 1600), ("bf16", 4, 2, 8, 1, 64, [64, 700], [1, 64], 700),
+    ("bf16", 8, 9, 8, 1, 20, [20 + 70 * b for b in range(9)], None, 600),
+    # more columns than compute units: four waves a workgroup, two column tiles where a cache has many of them
+    ("bf16", 4, 40, 8, 8, 1, [17 * b for b in range(40)], None, 700), ("f32", 8, 40, 8, 8, 1, [5 * b + 1 for b in range(40)], None, 200),
+    ("bf16", 8, 4, 40, 40, 1, [1300, 1, 700, 65], None, 1300), ("f32", 4, 4, 40, 40, 1, [1025, 64, 0, 513], None, 1100),
+    ("bf16", 4, 2, 32, 8, 130, [200, 140], [130, 77], 256), ("bf16", 8, 16, 8, 8, 70, [70 + 29 * b for b in range(16)], None, 530),
+    ("bf16", 4, 9, 24, 8, 40, [40 * b for b in range(9)], [40 - 4 * b for b in range(9)], 330),
+    ("bf16", 8, 1, 64, 4, 300, [290], None, 300)])
 def test_attend_matches_64_bits(ctx, case):
     dt, bits, Bn, Hq, Hkv, n, lens, counts, cap = case
     _say("cache attend %s" % (case,))
@@ -181,7 +195,9 @@ def test_attend_matches_64_bits(ctx, case):
     cnt = None if counts is None else torch.tensor(counts, dtype=torch.int32, device="cuda")
     ctx.tf_cache_attend(p, c.desc, q, o, cnt, ws)
     torch.cuda.synchronize()
-    _check_attention(o, ref.attend(q.double(), k, v, lens, counts or [n] * Bn, 128 ** -0.5), dt)
+    # a call whose columns (queries x heads of a KV head) are many tiles of 16
+    many = dt == "bf16" and n * (Hq // Hkv) > 16 and Bn * Hkv * -(-n * (Hq // Hkv) // 16) >= 512
+    _check_attention(o, ref.attend(q.double(), k, v, lens, counts or [n] * Bn, 128 ** -0.5), dt, many)
 
 
 def test_attend_strided_scaled_and_sharp(ctx):
