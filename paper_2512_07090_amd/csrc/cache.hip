@@ -176,12 +176,15 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const CacheReadArgs a)
 // Codes become bf16 exactly, two an instruction.  fp32 queries and their weights are sums of three bf16 parts, which
 // is exact.  Behind bf16 queries weights are two parts (2^-16), or, where a call has many columns (CT = 2), rounded
 // to bf16 once as the batched attention does, numerator and denominator alike: with two parts 2 x 256 queries of 32
-// / 8 heads x 6000 keys took 85 us, 68 so.
+// / 8 heads x 6000 keys took 85 us, 68 so.  Up to eight columns leave room for the second parts as columns of their
+// own (PAIRED: column c16 % 8, part c16 / 8), which halves the second product: 64 / 8 heads x 4000 14.2 -> 13.6 us,
+// 32 / 8 x 500 6.6 -> 6.4, 16 x 32 / 8 x up to 16384 50.4 -> 49.6.
 // (The scaled 4-bit product, which would take codes as they are, adds up with less than fp32: 1.5e-4 of the sum of
 // magnitudes was measured, and queries would have to be rounded to 8 bits.)
 // What bounds it: long caches the way of their bytes (8 x 32 heads x 8192 keys in 4 bits, 285 MB: 53 us, 5.3 TB/s),
-// many queries the instructions that convert and weigh (2 x 256 queries: 40.7 GFLOP at 0.59 PFLOP/s), short caches a
-// chain of latencies (32 / 8 heads x 500 keys: 6.7 us, of which a launch with one load takes 2.5).
+// many queries the instructions that convert and weigh (2 x 256 queries: 40.7 GFLOP in 62 us, vector and matrix
+// instructions hardly overlap), short caches a
+// chain of latencies (32 / 8 heads x 500 keys: 6.4 us, of which a launch with one load takes 2.5).
 // Parts of two values: three of them cut off, which is exact, or two rounded.
 template <int PARTS>
 __device__ __forceinline__ void split_pair(float a, float b, unsigned* w)
@@ -223,10 +226,12 @@ __device__ __forceinline__ void load_query(const float* p, bf16x8* f)
     for (int k = 0; k < PARTS; ++k) f[k] = __builtin_bit_cast(bf16x8, r[k]);
 }
 
-template <typename T, int BITS, int CT, int WAVES>
+template <typename T, int BITS, int CT, int WAVES, bool PAIRED>
 __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const CacheAttendArgs a)
 {
-    constexpr int kQ = sizeof(T) == 2 ? 1 : 3, kP = sizeof(T) != 2 ? 3 : CT == 1 ? 2 : 1;   // bf16 parts of a query, of a weight
+    static_assert(!PAIRED || (sizeof(T) == 2 && CT == 1), "");
+    constexpr int kQ = sizeof(T) == 2 ? 1 : 3, kP = PAIRED ? 1 : sizeof(T) != 2 ? 3 : CT == 1 ? 2 : 1;   // bf16 parts of a query, of a weight
+    constexpr bool kWholeSum = PAIRED || kP > 1;   // denominators from the weights before they are rounded
     constexpr int kRaw = BITS / 4;                                            // 16-byte loads of a lane and tile
     constexpr int kCols = 16 * CT, kThreads = 64 * WAVES, kRow = kHeadDim + 4;
     __shared__ __attribute__((aligned(16))) float o_part[WAVES][kCols][kRow];
@@ -288,7 +293,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
     int my_keys[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-        const int col = min(16 * ct + c16, cols - 1), q = tile * kCols + col;
+        const int col = min(16 * ct + (PAIRED ? c16 % 8 : c16), cols - 1), q = tile * kCols + col;
         my_keys[ct] = sees(token(col));
         const T* const row = static_cast<const T*>(a.q) + b * a.qs[0] + (hk * ratio + q % ratio) * a.qs[1] + q / ratio * a.qs[2] + 32 * g4;
 #pragma unroll
@@ -304,6 +309,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
     const uint8_t* const kb = static_cast<const uint8_t*>(a.k) + row_at;
     const uint8_t* const vb = static_cast<const uint8_t*>(a.v) + row_at;
 
+    const float second = PAIRED && c16 >= 8 ? -1.f : 0.f;
     f32x4 acc[CT][8];
     float mx[CT], sum[CT];
     f32x4 total[CT];   // (with whole weights: their sums on the matrix pipe, as rounded, in every register)
@@ -380,11 +386,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
 #pragma unroll
             for (int i = 1; i < 16; ++i) top = fmaxf(top, s[ct][i]);
             top = wave_group_max(top) * a.scale_log2e;
-            if (__any(top > mx[ct])) {
+            // (a reference that lags behind by up to 8 leaves weights of up to 256, and the sums are left alone: moved with
+            // every new maximum, one of a wave's columns has one in most pages: 2 x 256 queries 67.5 us, 62.5 so)
+            if (__any(top > mx[ct] + 8.f)) {
                 const float m_new = fmaxf(mx[ct], top), down = __builtin_amdgcn_exp2f(mx[ct] - m_new);
                 mx[ct] = m_new;
                 sum[ct] *= down;
-                if constexpr (kP == 1) total[ct] *= down;
+                if constexpr (!kWholeSum) total[ct] *= down;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) acc[ct][i] *= down;
             }
@@ -400,13 +408,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
                 for (int e = 0; e < 8; e += 2) {
                     const float p0 = __builtin_amdgcn_exp2f(fmaf(s[ct][8 * h + e], a.scale_log2e, -mx[ct]));
                     const float p1 = __builtin_amdgcn_exp2f(fmaf(s[ct][8 * h + e + 1], a.scale_log2e, -mx[ct]));
-                    if constexpr (kP > 1) sum[ct] += p0 + p1;
+                    if constexpr (kWholeSum) sum[ct] += p0 + p1;
                     unsigned w[kP];
-                    split_pair<kP>(p0, p1, w);
+                    if constexpr (PAIRED) {
+                        split_pair<1>(p0, p1, w);
+                        split_pair<1>(fmaf(__uint_as_float(w[0] << 16), second, p0), fmaf(__uint_as_float(w[0] & 0xffff0000u), second, p1), w);
+                    } else split_pair<kP>(p0, p1, w);
 #pragma unroll
                     for (int i = 0; i < kP; ++i) pf[ct][i][e / 2] = w[i];
                 }
-            if constexpr (kP == 1) {
+            if constexpr (!kWholeSum) {
                 const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
@@ -454,9 +465,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
     // the waves' results through LDS (register v of product i is column 8 (4 g4 + v) + i)
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-        if constexpr (kP == 1) sum[ct] = total[ct][0];
+        if constexpr (!kWholeSum) sum[ct] = total[ct][0];
         else sum[ct] = wave_group_sum(sum[ct]);
-        if (16 * ct + c16 < cols)
+        if (16 * ct + (PAIRED ? c16 % 8 : c16) < cols)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 float* dst = &o_part[wave][16 * ct + c16][8 * (4 * g4 + v)];
@@ -480,8 +491,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
             const float wt = __builtin_amdgcn_exp2f(stat[w][q][0] - m_all);
             den = fmaf(stat[w][q][1], wt, den);
             if (c == kHeadDim) continue;
-            v.x = fmaf(o_part[w][q][c], wt, v.x);
-            v.y = fmaf(o_part[w][q][c + 1], wt, v.y);
+            Float2 x = {o_part[w][q][c], o_part[w][q][c + 1]};
+            if constexpr (PAIRED) { x.x += o_part[w][q + 8][c]; x.y += o_part[w][q + 8][c + 1]; }
+            v.x = fmaf(x.x, wt, v.x);
+            v.y = fmaf(x.y, wt, v.y);
         }
         if (c == kHeadDim) v = {m_all, den};
         if (used > 1) put_shared(part0 + ((long long)sp * kCols + q) * kPartStride + c, v);
@@ -626,23 +639,25 @@ hipError_t launch_cache_attend(const CacheAttendArgs& in, const CachePlan& plan,
     a.tiles = plan.tiles; a.n_split = plan.split;
     a.tickets = (unsigned long long*)(a.part + tiles * a.n_split * 16 * plan.col_tiles * kPartStride);   // behind the partial results
     const unsigned grid = (unsigned)(tiles * a.n_split);
-#define TF_CACHE_ATTEND(T, BITS, CT, WAVES) cache_attend_kernel<T, BITS, CT, WAVES><<<dim3(grid), dim3(64 * WAVES), 0, s>>>(a)
-#define TF_CACHE_ATTEND_WAVES(T, BITS, CT)                                                        \
+#define TF_CACHE_ATTEND(T, BITS, CT, PAIRED)                                                      \
     do {                                                                                          \
-        if (plan.waves == 8) TF_CACHE_ATTEND(T, BITS, CT, 8);                                     \
-        else TF_CACHE_ATTEND(T, BITS, CT, 4);                                                     \
+        if (plan.waves == 8) cache_attend_kernel<T, BITS, CT, 8, PAIRED><<<dim3(grid), dim3(512), 0, s>>>(a); \
+        else cache_attend_kernel<T, BITS, CT, 4, PAIRED><<<dim3(grid), dim3(256), 0, s>>>(a);     \
     } while (0)
+    const bool paired = (long long)a.n * (a.Hq / a.Hkv) <= 8;
     if (dtype == 0) {
-        if (bits == 4) TF_CACHE_ATTEND_WAVES(float, 4, 1);
-        else TF_CACHE_ATTEND_WAVES(float, 8, 1);
-    } else if (plan.col_tiles == 1) {
-        if (bits == 4) TF_CACHE_ATTEND_WAVES(uint16_t, 4, 1);
-        else TF_CACHE_ATTEND_WAVES(uint16_t, 8, 1);
+        if (bits == 4) TF_CACHE_ATTEND(float, 4, 1, false);
+        else TF_CACHE_ATTEND(float, 8, 1, false);
+    } else if (plan.col_tiles == 2) {
+        if (bits == 4) TF_CACHE_ATTEND(uint16_t, 4, 2, false);
+        else TF_CACHE_ATTEND(uint16_t, 8, 2, false);
+    } else if (paired) {
+        if (bits == 4) TF_CACHE_ATTEND(uint16_t, 4, 1, true);
+        else TF_CACHE_ATTEND(uint16_t, 8, 1, true);
     } else {
-        if (bits == 4) TF_CACHE_ATTEND_WAVES(uint16_t, 4, 2);
-        else TF_CACHE_ATTEND_WAVES(uint16_t, 8, 2);
+        if (bits == 4) TF_CACHE_ATTEND(uint16_t, 4, 1, false);
+        else TF_CACHE_ATTEND(uint16_t, 8, 1, false);
     }
-#undef TF_CACHE_ATTEND_WAVES
 #undef TF_CACHE_ATTEND
     return hipGetLastError();
 }
