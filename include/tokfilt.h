@@ -342,7 +342,7 @@ typedef struct {
     void *k, *v;       /* DEVICE, tf_cache_bytes() each, 16-byte aligned */
     int32_t *len;      /* DEVICE [batch]: rows held */
     int32_t *overflow; /* DEVICE [batch], or NULL: set to 1 where a row did not fit */
-    int32_t capacity;  /* rows per (batch, head), >= 1 */
+    int32_t capacity;  /* rows per (batch, head), 1 .. 2^30 */
     int32_t format;    /* tf_cache_format */
 } tf_cache;
 

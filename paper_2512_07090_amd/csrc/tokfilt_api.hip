@@ -34,6 +34,7 @@ namespace {
 
 constexpr int kMaxTimedCalls = 256;
 constexpr int kMaxKvHeads = 128;  // LDS staging of the fusion kernel
+constexpr int kMaxQuantRows = 1 << 30;  // of a quantised cache: row numbers a little beyond it are formed in 32 bits
 constexpr int kMaxOnlineSeq = 1 << 24;  // the online decision's float counter of skipped tokens is exact up to here
 
 tf_status fail(tf_ctx* c, tf_status s, const char* fmt, ...) __attribute__((format(printf, 3, 4)));
@@ -222,6 +223,13 @@ tf_status check_format(tf_ctx* ctx, int32_t format)
     return fail(ctx, TF_ERR_INVALID_ARG, "unknown cache format");
 }
 
+tf_status check_state_format(tf_ctx* ctx, const tf_decode_state* st, int32_t format)
+{
+    const tf_status s = check_format(ctx, format);
+    if (s == TF_OK && st && st->capacity > kMaxQuantRows) return fail(ctx, TF_ERR_UNSUPPORTED, "cache too large");
+    return s;
+}
+
 // validation shared by the calls on a cache in 4 or 8 bits
 tf_status check_cache(tf_ctx* ctx, const tf_params* p, const tf_cache* c)
 {
@@ -235,7 +243,7 @@ tf_status check_cache(tf_ctx* ctx, const tf_params* p, const tf_cache* c)
     if (!c->k || !c->v || !c->len) return fail(ctx, TF_ERR_INVALID_ARG, "k, v and len of the cache must not be NULL");
     if (c->capacity < 1) return fail(ctx, TF_ERR_INVALID_ARG, "cache: capacity must be >= 1");
     if (misaligned(c->k) || misaligned(c->v)) return fail(ctx, TF_ERR_INVALID_ARG, "caches must be 16-byte aligned");
-    if ((int64_t)p->batch * p->n_kv_heads * (int64_t)c->capacity > ((int64_t)1 << 40) / tf::kHeadDim)
+    if (c->capacity > kMaxQuantRows || (int64_t)p->batch * p->n_kv_heads * (int64_t)c->capacity > ((int64_t)1 << 40) / tf::kHeadDim)
         return fail(ctx, TF_ERR_UNSUPPORTED, "cache too large");
     return TF_OK;
 }
@@ -642,6 +650,9 @@ tf_status tf_norm_rotate(tf_ctx* ctx, const tf_params* p, const tf_rotary* r, co
                 return fail(ctx, TF_ERR_INVALID_ARG, "in place the strides of Q and of its output must be equal");
     if ((Q && folded(p->o_stride, p->batch, p->n_q_heads)) || (K && folded(p->kv_stride, p->batch, p->n_kv_heads)))
         return fail(ctx, TF_ERR_INVALID_ARG, "an output must not have a stride of 0");
+    // a workgroup for 16 heads of one to four tokens
+    if ((int64_t)p->batch * p->seq * ((p->n_q_heads + 15) / 16 + (p->n_kv_heads + 15) / 16) >= ((int64_t)1 << 31))
+        return fail(ctx, TF_ERR_UNSUPPORTED, "too many rows for one call");
     st = use_device(ctx);
     if (st != TF_OK) return st;
     tf::NormRotateArgs a;
@@ -656,7 +667,7 @@ tf_status tf_norm_rotate(tf_ctx* ctx, const tf_params* p, const tf_rotary* r, co
 size_t tf_cache_bytes(const tf_params* p, int32_t format, int32_t capacity)
 {
     const char* why;
-    if (check_shape(p, &why) != TF_OK || capacity < 1 || (format != TF_CACHE_FP4 && format != TF_CACHE_FP8)) return 0;
+    if (check_shape(p, &why) != TF_OK || capacity < 1 || capacity > kMaxQuantRows || (format != TF_CACHE_FP4 && format != TF_CACHE_FP8)) return 0;
     return tf::cache_bytes(format, (long long)p->batch * p->n_kv_heads, capacity);
 }
 
@@ -741,7 +752,7 @@ tf_status tf_decode_prefill_q(tf_ctx* ctx, const tf_params* p, float eta, float 
                               void* stream)
 {
     if (!ctx) return TF_ERR_INVALID_ARG;
-    const tf_status st = check_format(ctx, format);
+    const tf_status st = check_state_format(ctx, state, format);
     if (st != TF_OK) return st;
     return prefill(ctx, p, eta, tau0, state, format, Q, K, V, keep, kept_idx, count, fused, O, ws, ws_bytes, stream);
 }
@@ -751,7 +762,7 @@ tf_status tf_decode_step_q(tf_ctx* ctx, const tf_params* p, float eta, const tf_
                            size_t ws_bytes, void* stream)
 {
     if (!ctx) return TF_ERR_INVALID_ARG;
-    tf_status st = check_format(ctx, format);
+    tf_status st = check_state_format(ctx, state, format);
     if (st != TF_OK) return st;
     tf::DecodeArgs a;
     st = decode_args(ctx, p, state, &a);

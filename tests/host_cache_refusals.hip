@@ -38,7 +38,8 @@ int main()
         tf_cache_bytes(&p, TF_CACHE_FP4, 65) != 8 * 4352 || tf_cache_bytes(&p, TF_CACHE_FP8, 64) != 4 * 8448) { ++bad; printf("sizes\n"); }
     if (tf_cache_bytes(&p, 0, 64) || tf_cache_bytes(&p, 16, 64) || tf_cache_bytes(&p, 4, 0) || tf_cache_bytes(nullptr, 4, 64) ||
         tf_cache_workspace_bytes(nullptr)) { ++bad; printf("sizes of nothing\n"); }
-    if (tf_cache_bytes(&p, TF_CACHE_FP8, 0x7fffffff) != 4ull * 33554432 * 8448) { ++bad; printf("large size\n"); }
+    if (tf_cache_bytes(&p, TF_CACHE_FP8, 1 << 30) != 4ull * 16777216 * 8448) { ++bad; printf("large size\n"); }
+    if (tf_cache_bytes(&p, TF_CACHE_FP8, (1 << 30) + 1) != 0) { ++bad; printf("size of too many rows\n"); }
     for (int b : {1, 3, 64}) for (int n : {1, 5, 300}) {
         const tf_params x = shape(b, 32, 8, n, TF_BF16);
         const size_t w = tf_cache_workspace_bytes(&x);
@@ -68,7 +69,8 @@ int main()
     expect(c, write(c, &p, &good, (char*)K + 2, V, 4), inv, "write, alignment");
     expect(c, write(c, &p, &good, K, V, 0), inv, "write, m = 0");
     expect(c, write(c, &p, &good, K, V, 5), inv, "write, m > seq");
-    { tf_cache d = good; d.capacity = 0x7fffffff; tf_params x = shape(65535, 128, 128, 1, TF_F32);
+    { tf_cache d = good; d.capacity = (1 << 30) + 1; expect(c, write(c, &p, &d, K, V, 4), TF_ERR_UNSUPPORTED, "write, too many rows of a cache"); }
+    { tf_cache d = good; d.capacity = 1 << 30; tf_params x = shape(65535, 128, 128, 1, TF_F32);
       expect(c, write(c, &x, &d, K, V, 1), TF_ERR_UNSUPPORTED, "write, too large a cache"); }
     { tf_params x = shape(128, 128, 128, 1 << 23, TF_F32);
       expect(c, write(c, &x, &good, K, V, 1 << 23), TF_ERR_UNSUPPORTED, "write, too many rows");
@@ -91,6 +93,8 @@ int main()
         expect(c, tf_decode_step_q(c, &p, 0.f, &st, f, Q, K, V, O, (uint8_t*)four, (float*)four, ws, sizeof ws, nullptr), inv, "step, format");
         expect(c, tf_decode_prefill_q(c, &p, 0.f, 0.f, &st, f, Q, K, V, (uint8_t*)four, four, four, (float*)four, O, ws, sizeof ws, nullptr), inv, "prefill, format");
     }
+    { tf_decode_state big = st; big.capacity = (1 << 30) + 1;
+      expect(c, tf_decode_step_q(c, &p, 0.f, &big, 4, Q, K, V, O, (uint8_t*)four, (float*)four, ws, sizeof ws, nullptr), TF_ERR_UNSUPPORTED, "step, too many rows"); }
     expect(nullptr, tf_decode_step_q(nullptr, &p, 0.f, &st, 4, Q, K, V, O, (uint8_t*)four, (float*)four, ws, sizeof ws, nullptr), inv, "step, no context");
     expect(nullptr, tf_decode_prefill_q(nullptr, &p, 0.f, 0.f, &st, 4, Q, K, V, (uint8_t*)four, four, four, (float*)four, O, ws, sizeof ws, nullptr), inv, "prefill, no context");
 
@@ -120,6 +124,7 @@ int main()
     expect(c, rotate(&r, &p, Q, K, nullptr, V), inv, "rotate, no output");
     expect(c, rotate(&r, &p, Q, nullptr, O, V), inv, "rotate, no input");
     expect(c, rotate(&r, &p, (char*)Q + 2, K, O, V), inv, "rotate, alignment");
+    { tf_params x = shape(1024, 65535, 1, 1 << 20, TF_F32); expect(c, rotate(&r, &x, Q, K, O, V), TF_ERR_UNSUPPORTED, "rotate, too many rows"); }
     { tf_params x = p; x.o_stride[0] *= 2; expect(c, rotate(&r, &x, Q, K, Q, V), inv, "rotate, in place elsewhere"); }
     { tf_params x = p; x.kv_stride[0] = 0; expect(c, rotate(&r, &x, Q, K, O, V), inv, "rotate, folded"); }
 

@@ -215,6 +215,32 @@ def test_attend_strided_scaled_and_sharp(ctx):
     assert torch.isnan(o.as_strided((Bn, n, Hq, 8), (n * Hq * 136, Hq * 136, 136, 1), o.storage_offset() + 128)).all()
 
 
+@pytest.mark.parametrize("case", [("bf16", 2, 8, 2, 3), ("bf16", 2, 8, 2, 12), ("f32", 2, 4, 2, 5), ("bf16", 20, 16, 8, 40)])
+def test_padding_may_hold_anything(ctx, case):
+    """Queries from count on, and rows of the cache behind its length, are NaN and infinities: no trace of them."""
+    dt, Bn, Hq, Hkv, n = case
+    _say("cache attend padding %s" % (case,))
+    lens, counts = [200 + 13 * b for b in range(Bn)], [n - 1 - b % (n - 1) for b in range(Bn)]
+    p = _params(dt, Bn, Hq, Hkv, n)
+    c, k, v = _quant_cache(p, dt, 8, Bn, Hkv, lens, 520, 33)
+    q = _rows((Bn, Hq, n, 128), dt, 34, 0.2)
+    clean = q.clone()
+    for b in range(Bn):
+        q[b, :, counts[b]:] = float("nan") if b % 2 else float("inf")
+    cnt = torch.tensor(counts, dtype=torch.int32, device="cuda")
+    ws = torch.full((B.tf_cache_workspace_bytes(p),), 0xFF, dtype=torch.uint8, device="cuda")
+    outs = []
+    for x in (q, clean):
+        o = torch.full_like(q, float("nan"))
+        ctx.tf_cache_attend(p, c.desc, x, o, cnt, ws)
+        outs.append(o)
+    torch.cuda.synchronize()
+    assert torch.equal(*outs)
+    for b in range(Bn):
+        assert not outs[0][b, :, counts[b]:].any()
+    assert torch.isfinite(outs[0].float()).all()
+
+
 def test_attend_row_does_not_depend_on_its_neighbours(ctx):
     Bn, Hq, Hkv, n, cap = 5, 8, 2, 4, 1500
     _say("cache attend neighbours")
@@ -294,6 +320,77 @@ def test_calls_on_two_streams_and_from_replayed_graphs(ctx):
         assert torch.equal(o, want[i]) and torch.equal(o2, want[i]), i
         assert c.len.tolist() == [501 + i] * Bn
     assert torch.equal(c.len, cw.len)
+
+
+def test_two_graphs_share_a_workspace(ctx):
+    """Two layers captured apart, with other lengths and other numbers of slices, replayed in turn over one workspace."""
+    Bn, Hq, Hkv, cap = 2, 8, 2, 3000
+    _say("cache two graphs")
+    layers, graphs, s = [], [], torch.cuda.Stream()
+    ws = None
+    for n, lens in ((1, [2900, 40]), (5, [700, 3000])):
+        p = _params("bf16", Bn, Hq, Hkv, n)
+        c, k, v = _quant_cache(p, "bf16", 4, Bn, Hkv, lens, cap, 70 + n)
+        q = _rows((Bn, Hq, n, 128), "bf16", 80 + n)
+        o, want = torch.empty_like(q), torch.empty_like(q)
+        ws = torch.full((2 * B.tf_cache_workspace_bytes(p),), 0xFF, dtype=torch.uint8, device="cuda") if ws is None else ws
+        assert ws.numel() >= B.tf_cache_workspace_bytes(p)
+        ctx.tf_cache_attend(p, c.desc, q, want, None, ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            ctx.tf_cache_attend(p, c.desc, q, o, None, ws)
+        layers.append((o, want, c, q))
+        graphs.append(g)
+    for turn in (0, 1, 0, 0, 1, 1, 0):
+        layers[turn][0].fill_(float("nan"))
+        graphs[turn].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(layers[turn][0], layers[turn][1]), turn
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_a_request_from_projections_to_decoded_tokens(ctx, bits):
+    """As a server runs them: norm and rotation of a prompt, the filtered prompt into a quantised cache, then for each token
+    norm and rotation at the position the state has counted to, and the filtered step."""
+    Bn, Hq, Hkv, n, steps, eta, tau0 = 2, 8, 2, 120, 24, 0.05, 0.4
+    _say("cache request %d" % bits)
+    w = synth.scaled(synth.workload(0), batch=Bn, seq=n + steps, n_q_heads=Hq, n_kv_heads=Hkv, dtype="bf16")
+    q, k, v, _ = (x.cuda() if isinstance(x, torch.Tensor) else x for x in synth.make_qkv(w))
+    freq = torch.exp(torch.arange(64, dtype=torch.float64, device="cuda") * (-np.log(1e4) / 64))
+    wq, wk = (1 + 0.1 * torch.randn(128, device="cuda") for _ in range(2))
+    whole = B.make_params(tuple(q.shape), tuple(k.shape), q.dtype, 0.5, 4)
+    qr, kr = torch.empty_like(q), torch.empty_like(k)          # all tokens at once
+    ctx.tf_norm_rotate(whole, B.make_rotary(freq, 128, wq, wk), q, k, qr, kr)
+    p = B.make_params((Bn, Hq, n, 128), (Bn, Hkv, n, 128), q.dtype, 0.5, 4)
+    buf = B.DecodeBuffers(p, n + steps, cache_format=bits)
+    a = [x[:, :, :n].contiguous() for x in (q, k, v)]
+    ctx.tf_norm_rotate(p, B.make_rotary(freq, 128, wq, wk), a[0], a[1], a[0], a[1])
+    keep, count = torch.empty((Bn, n), dtype=torch.uint8, device="cuda"), torch.empty(Bn, dtype=torch.int32, device="cuda")
+    idx, fused, O = torch.empty((Bn, n), dtype=torch.int32, device="cuda"), torch.empty((Bn, n), device="cuda"), torch.empty_like(a[0])
+    ctx.tf_decode_prefill_q(p, eta, tau0, buf.state, bits, *a, keep, idx, count, fused, O,
+                            torch.empty(B.tf_workspace_bytes(p), dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    assert torch.equal(a[0], qr[:, :, :n]) and torch.equal(a[1], kr[:, :, :n])
+    kept = [keep[b].nonzero().flatten().tolist() for b in range(Bn)]
+    one = B.make_params((Bn, Hq, 1, 128), (Bn, Hkv, 1, 128), q.dtype, 0.5, 4)
+    rot = B.make_rotary(freq, 128, wq, wk, start=buf.seen)
+    attended = 0
+    for t in range(n, n + steps):
+        a = [x[:, :, t].contiguous() for x in (q, k, v)]
+        ctx.tf_norm_rotate(one, rot, a[0], a[1], a[0], a[1])
+        ctx.tf_decode_step_q(p, eta, buf.state, bits, *a, buf.o, buf.skip, buf.fused, buf.ws)
+        torch.cuda.synchronize()
+        assert torch.equal(a[0], qr[:, :, t]) and torch.equal(a[1], kr[:, :, t])
+        for b in range(Bn):
+            if buf.skip[b]:
+                assert not buf.o[b].any()
+                continue
+            kept[b].append(t)
+            attended += 1
+            kk, vv = (torch.from_numpy(ref.values(*ref.quantise(_f64(x[b][:, kept[b]]), bits), bits)).cuda()[None] for x in (kr, v))
+            _check_attention(buf.o[b:b + 1, :, None], ref.attend(a[0][b:b + 1, :, None].double(), kk, vv, [len(kept[b])], [1], 128 ** -0.5), "bf16")
+    assert 0 < attended < steps * Bn and buf.cache_len.tolist() == [len(x) for x in kept]
 
 
 @pytest.mark.parametrize("case", [   # dtype, bits, batch, query heads, KV heads, prompt, steps, fusion, gamma
