@@ -514,34 +514,35 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
     if (drawn != used - 1) return;
     // (a replayed graph calls by the same number again)
     if (threadIdx.x == 0) __hip_atomic_store(ticket, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    for (int q = wave; q < cols; q += WAVES) {
-        Float2 own = {kLowest, 0.f};
-        if (lane < used) own = get_shared(part0 + ((long long)lane * kCols + q) * kPartStride + kHeadDim);
-        float m_all = own.x;
-#pragma unroll
-        for (int step = 1; step < 64; step *= 2) m_all = fmaxf(m_all, __shfl_xor(m_all, step));
-        const float wt = __builtin_amdgcn_exp2f(own.x - m_all);
-        float den = own.y * wt;
-#pragma unroll
-        for (int step = 1; step < 64; step *= 2) den += __shfl_xor(den, step);
-        weight[q][lane] = wt;
-        if (lane == 0) weight[q][kDecodeMaxSplit] = den;
-    }
-    __syncthreads();
     auto merge = [&](auto batch) {
         constexpr int kBatch = decltype(batch)::value;
-        for (int i = threadIdx.x; i < cols * (kHeadDim / 2); i += kThreads) {
+        const int pairs = cols * (kHeadDim / 2);
+        // (the first slices' numerators are requested before their weights are known)
+        Float2 x[kBatch];
+        auto fetch = [&](int i, int l) {
+            const float* p = part0 + i / (kHeadDim / 2) * kPartStride + 2 * (i % (kHeadDim / 2));
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) x[u] = get_shared(p + (long long)min(l + u, used - 1) * kCols * kPartStride);
+        };
+        if ((int)threadIdx.x < pairs) fetch(threadIdx.x, 0);
+        for (int q = wave; q < cols; q += WAVES) {
+            Float2 own = {kLowest, 0.f};
+            if (lane < used) own = get_shared(part0 + ((long long)lane * kCols + q) * kPartStride + kHeadDim);
+            const float m_all = wave_group_max(row16_max(own.x)), wt = __builtin_amdgcn_exp2f(own.x - m_all);
+            const float den = wave_group_sum(row16_sum(own.y * wt));
+            weight[q][lane] = lane < used ? wt : 0.f;
+            if (lane == 0) weight[q][kDecodeMaxSplit] = den;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < pairs; i += kThreads) {
             const int q = i / (kHeadDim / 2), c = 2 * (i % (kHeadDim / 2));
             Float2 num = {0.f, 0.f};
             for (int l = 0; l < used; l += kBatch) {
-                Float2 x[kBatch];
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u) x[u] = get_shared(part0 + ((long long)min(l + u, used - 1) * kCols + q) * kPartStride + c);
+                if (l > 0 || i >= kThreads) fetch(i, l);
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) {
-                    const float wt = l + u < used ? weight[q][l + u] : 0.f;
-                    num.x = fmaf(x[u].x, wt, num.x);
-                    num.y = fmaf(x[u].y, wt, num.y);
+                    num.x = fmaf(x[u].x, weight[q][l + u], num.x);
+                    num.y = fmaf(x[u].y, weight[q][l + u], num.y);
                 }
             }
             const float den = weight[q][kDecodeMaxSplit];
