@@ -243,34 +243,36 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
     // The tiles of a cache go to one die, whose L2 they then share: workgroups are dealt out to the dies in turn, so
     // eight caches a time, one for each; what is left over of them is spread.
     int at = blockIdx.x;
-    int bh = at / a.n_split / a.tiles;
+    int bh = quotient(quotient(at, a.by_split), a.by_tiles);
     if (a.tiles > 1) {
-        const int group = a.n_split * a.tiles, caches = a.B * a.Hkv;
-        if (const int eight = at / (8 * group); 8 * eight + 8 <= caches) {
-            bh = 8 * eight + at % 8;
-            at = at % (8 * group) / 8;
+        const int group = a.n_split * a.tiles, eight = bh >> 3;
+        if (8 * eight + 8 <= a.B * a.Hkv) {
+            const int in = at - 8 * eight * group;
+            bh = 8 * eight + (in & 7);
+            at = in >> 3;
         }
     }
-    const int sp = at % a.n_split, tile = at / a.n_split % a.tiles;
-    const int b = bh / a.Hkv, hk = bh % a.Hkv;
-    const int ratio = a.Hq / a.Hkv;
+    const int slice_of = quotient(at, a.by_split), sp = at - slice_of * a.n_split;
+    const int tile = slice_of - quotient(slice_of, a.by_tiles) * a.tiles;
+    const int b = quotient(bh, a.by_hkv), hk = bh - b * a.Hkv;
+    const int ratio = a.by_ratio.by;
     const int held = min(max(a.len[b], 0), a.capacity);
     const int there = a.skip && a.skip[b] ? 0 : a.count ? min(max(a.count[b], 0), a.n) : a.n;   // queries of this row
     // keys that query t sees (none: a zero row)
     auto sees = [&](int t) { return t < there ? max(held - there + t + 1, 0) : 0; };
     const int cols = min(kCols, a.n * ratio - tile * kCols);
-    auto token = [&](int col) { return (tile * kCols + col) / ratio; };
+    auto token = [&](int col) { return quotient(tile * kCols + col, a.by_ratio); };
     const int first_t = token(0), last_t = min(token(cols - 1), there - 1);
     const int keys = last_t < first_t ? 0 : sees(last_t);        // of any of the columns
     T* const out = static_cast<T*>(a.o) + b * a.os[0];
     auto out_row = [&](int col) {
-        const int q = tile * kCols + col;
-        return out + (hk * ratio + q % ratio) * a.os[1] + q / ratio * a.os[2];
+        const int q = tile * kCols + col, t = quotient(q, a.by_ratio);
+        return out + (hk * ratio + q - t * ratio) * a.os[1] + t * a.os[2];
     };
     // The slices of a row follow from its own length.  Up to 512 keys are one (8.1 us for 500 in two slices, 6.7 in one),
     // up to eight slices of 256 are merged in one go (2000 keys 9.6 -> 8.3), beyond that they are longer (8000: 11.9 -> 10.6).
     const int least = held <= 512 ? 512 : held <= 2048 ? 256 : 512;
-    const int chunk = max(least, ((held + a.n_split - 1) / a.n_split + kPageRows - 1) / kPageRows * kPageRows);
+    const int chunk = max(least, (quotient(held + a.n_split - 1, a.by_split) + kPageRows - 1) / kPageRows * kPageRows);
     const int used = (keys + chunk - 1) / chunk;
     if (sp >= used) {
         if (used == 0 && sp == 0)
@@ -293,9 +295,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
     int my_keys[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-        const int col = min(16 * ct + (PAIRED ? c16 % 8 : c16), cols - 1), q = tile * kCols + col;
-        my_keys[ct] = sees(token(col));
-        const T* const row = static_cast<const T*>(a.q) + b * a.qs[0] + (hk * ratio + q % ratio) * a.qs[1] + q / ratio * a.qs[2] + 32 * g4;
+        const int col = min(16 * ct + (PAIRED ? c16 % 8 : c16), cols - 1), q = tile * kCols + col, t = quotient(q, a.by_ratio);
+        my_keys[ct] = sees(t);
+        const T* const row = static_cast<const T*>(a.q) + b * a.qs[0] + (hk * ratio + q - t * ratio) * a.qs[1] + t * a.qs[2] + 32 * g4;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             bf16x8 f[kQ];
@@ -638,6 +640,7 @@ hipError_t launch_cache_attend(const CacheAttendArgs& in, const CachePlan& plan,
     CacheAttendArgs a = in;
     const long long tiles = (long long)a.B * a.Hkv * plan.tiles;
     a.tiles = plan.tiles; a.n_split = plan.split;
+    a.by_ratio = divisor(a.Hq / a.Hkv); a.by_split = divisor(a.n_split); a.by_tiles = divisor(a.tiles); a.by_hkv = divisor(a.Hkv);
     a.tickets = (unsigned long long*)(a.part + tiles * a.n_split * 16 * plan.col_tiles * kPartStride);   // behind the partial results
     const unsigned grid = (unsigned)(tiles * a.n_split);
 #define TF_CACHE_ATTEND(T, BITS, CT, PAIRED)                                                      \

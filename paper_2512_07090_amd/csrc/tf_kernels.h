@@ -137,6 +137,15 @@ struct CacheReadArgs {
     int B, Hkv, n, capacity, cache_pages, pages;
     long long kvs[3];
 };
+// Division of 0 .. 2^31 - 1 by a number known on the host: a product, an addition and a shift on the device.
+struct Divisor { unsigned by, mul, shift; };
+inline Divisor divisor(unsigned by)
+{
+    Divisor d = {by, 0, 0};
+    while ((1ull << d.shift) < by) ++d.shift;
+    d.mul = (unsigned)((((1ull << d.shift) - by) << 32) / by + 1);
+    return d;
+}
 struct CacheAttendArgs {
     const void *q, *k, *v;
     void* o;
@@ -146,6 +155,7 @@ struct CacheAttendArgs {
     unsigned long long* tickets;                    // a call's number and its slices that are done
     unsigned long long call;                        // < 2^48, not 0, another one each call
     int B, Hq, Hkv, n, tiles, capacity, cache_pages, n_split;
+    Divisor by_ratio, by_split, by_tiles, by_hkv;   // (set by the launcher)
     float scale_log2e;
     long long qs[3], os[3];
 };
@@ -165,6 +175,8 @@ hipError_t launch_probe_mfma(int iters, void* sink, int n_cu, hipStream_t s);
 
 // ---- small device helpers -----------------------------------------------------------------
 #ifdef __HIPCC__
+__device__ __forceinline__ int quotient(int x, const Divisor& d) { return (int)((__umulhi((unsigned)x, d.mul) + (unsigned)x) >> d.shift); }
+
 template <int CTRL>
 __device__ __forceinline__ float dpp_mov(float v)
 {
