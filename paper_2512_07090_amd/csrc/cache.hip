@@ -331,6 +331,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
 #pragma unroll
             for (int i = 0; i < kRaw; ++i) k_raw[t][i] = *reinterpret_cast<const u32x4*>(p + key_code_at<BITS>(16 * t + c16, 4 * g4) + 16 * i);
         k_scale = *reinterpret_cast<const unsigned*>(p + page_codes<BITS>() + 4 * lane);
+        asm volatile("" ::: "memory");
     };
     auto request_v = [&](int j) {
         const uint8_t* p = vb + (long long)(j / kPageRows) * page_bytes<BITS>();
@@ -339,10 +340,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
 #pragma unroll
             for (int i = 0; i < kRaw; ++i) v_raw[t][i] = *reinterpret_cast<const u32x4*>(p + value_code_at<BITS>(16 * t + 4 * g4, c16) + 16 * i);
         v_scale = *reinterpret_cast<const u32x4*>(p + page_codes<BITS>() + (4 * g4 + (c16 >> 2)) * 16);
+        asm volatile("" ::: "memory");
     };
-    int j = lo + kPageRows * wave;
-    if (j < hi) { request_k(j); request_v(j); }
-    for (; j < hi; j += WAVES * kPageRows) {
+    auto weigh_page = [&](int j, auto more) {
         // scores of the page, a tile of 16 keys after the other
         float s[CT][16];
 #pragma unroll
@@ -371,8 +371,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
 #pragma unroll
                 for (int v = 0; v < 4; ++v) s[ct][4 * t + v] = d[ct][v];
         }
-        const bool more = j + WAVES * kPageRows < hi;
-        if (more) request_k(j + WAVES * kPageRows);
+        if constexpr (more) request_k(j + WAVES * kPageRows);
         if (j + kPageRows > all_see) {
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
@@ -461,7 +460,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
                 }
             }
         }
-        if (more) request_v(j + WAVES * kPageRows);
+        if constexpr (more) request_v(j + WAVES * kPageRows);
+    };
+    int j = lo + kPageRows * wave;
+    if (j < hi) {
+        request_k(j);
+        request_v(j);
+        for (; j + WAVES * kPageRows < hi; j += WAVES * kPageRows) weigh_page(j, std::true_type());
+        weigh_page(j, std::false_type());
     }
 
     // the waves' results through LDS (register v of product i is column 8 (4 g4 + v) + i)
