@@ -167,6 +167,12 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const CacheReadArgs a)
     }
 }
 
+__device__ __forceinline__ void store_pair(uint16_t* p, float x, float y)
+{
+    *reinterpret_cast<unsigned*>(p) = __builtin_bit_cast(unsigned, bf16x2{(__bf16)x, (__bf16)y});
+}
+__device__ __forceinline__ void store_pair(float* p, float x, float y) { *reinterpret_cast<float2*>(p) = make_float2(x, y); }
+
 // ---- attention -----------------------------------------------------------------------------
 // A column is one query of one head: token t, head g of the `ratio` that share a KV head, column t * ratio + g.
 // A workgroup takes CT tiles of 16 columns and one slice of the row's keys, a wave a page of 64 keys at a time.
@@ -236,7 +242,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
     constexpr int kCols = 16 * CT, kThreads = 64 * WAVES, kRow = kHeadDim + 4;
     __shared__ __attribute__((aligned(16))) float o_part[WAVES][kCols][kRow];
     __shared__ float stat[WAVES][kCols][2];
-    __shared__ float weight[kCols][kDecodeMaxSplit + 1];
     __shared__ int drawn;
     const int lane = threadIdx.x & 63, c16 = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -398,8 +403,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
                 for (int i = 0; i < 8; ++i) acc[ct][i] *= down;
             }
         }
-        // keys behind the last: whatever lies there, their weights are zero and so are their values
-        const bool clear = j + kPageRows > hi;
+        // keys behind the last (of the wave's last page): whatever lies there, their weights are zero and so are their values
+        const bool clear = !more && j + kPageRows > hi;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             u32x4 pf[CT][kP];
@@ -485,31 +490,29 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
         if (lane < 16) { stat[wave][16 * ct + lane][0] = mx[ct]; stat[wave][16 * ct + lane][1] = sum[ct]; }
     }
     __syncthreads();
-    constexpr int kPairs = kPartStride / 2;   // the last one: running max, sum
+    // From here on a wave takes whole columns, a lane two neighbouring values.
     float* const part0 = a.part + ((long long)bh * a.tiles + tile) * a.n_split * kCols * kPartStride;   // [slice][column]
-    for (int i = threadIdx.x; i < cols * kPairs; i += kThreads) {
-        const int q = i / kPairs, c = 2 * (i - q * kPairs);
-        float m_all = kLowest;
+    for (int q = wave; q < cols; q += WAVES) {
+        float m_all = kLowest, den = 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) m_all = fmaxf(m_all, stat[w][q][0]);
         Float2 v = {0.f, 0.f};
-        float den = 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
             const float wt = __builtin_amdgcn_exp2f(stat[w][q][0] - m_all);
             den = fmaf(stat[w][q][1], wt, den);
-            if (c == kHeadDim) continue;
-            Float2 x = {o_part[w][q][c], o_part[w][q][c + 1]};
-            if constexpr (PAIRED) { x.x += o_part[w][q + 8][c]; x.y += o_part[w][q + 8][c + 1]; }
+            Float2 x = {o_part[w][q][2 * lane], o_part[w][q][2 * lane + 1]};
+            if constexpr (PAIRED) { x.x += o_part[w][q + 8][2 * lane]; x.y += o_part[w][q + 8][2 * lane + 1]; }
             v.x = fmaf(x.x, wt, v.x);
             v.y = fmaf(x.y, wt, v.y);
         }
-        if (c == kHeadDim) v = {m_all, den};
-        if (used > 1) put_shared(part0 + ((long long)sp * kCols + q) * kPartStride + c, v);
-        else if (c < kHeadDim) {
+        if (used == 1) {
             const bool some = sees(token(q)) > 0;
-            store_out(out_row(q) + c, some ? v.x / den : 0.f);
-            store_out(out_row(q) + c + 1, some ? v.y / den : 0.f);
+            store_pair(out_row(q) + 2 * lane, some ? v.x / den : 0.f, some ? v.y / den : 0.f);
+        } else {
+            float* const p = part0 + ((long long)sp * kCols + q) * kPartStride;
+            put_shared(p + 2 * lane, v);
+            if (lane == 0) put_shared(p + kHeadDim, Float2{m_all, den});
         }
     }
     if (used == 1) return;
@@ -524,39 +527,32 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
     if (threadIdx.x == 0) __hip_atomic_store(ticket, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     auto merge = [&](auto batch) {
         constexpr int kBatch = decltype(batch)::value;
-        const int pairs = cols * (kHeadDim / 2);
-        // (the first slices' numerators are requested before their weights are known)
-        Float2 x[kBatch];
-        auto fetch = [&](int i, int l) {
-            const float* p = part0 + i / (kHeadDim / 2) * kPartStride + 2 * (i % (kHeadDim / 2));
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) x[u] = get_shared(p + (long long)min(l + u, used - 1) * kCols * kPartStride);
-        };
-        if ((int)threadIdx.x < pairs) fetch(threadIdx.x, 0);
         for (int q = wave; q < cols; q += WAVES) {
+            const float* const p = part0 + q * kPartStride;
+            // (the first slices' numerators are requested before their weights are known)
+            Float2 x[kBatch];
+            auto fetch = [&](int l) {
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) x[u] = get_shared(p + (long long)min(l + u, used - 1) * kCols * kPartStride + 2 * lane);
+            };
+            fetch(0);
             Float2 own = {kLowest, 0.f};
-            if (lane < used) own = get_shared(part0 + ((long long)lane * kCols + q) * kPartStride + kHeadDim);
-            const float m_all = wave_group_max(row16_max(own.x)), wt = __builtin_amdgcn_exp2f(own.x - m_all);
+            if (lane < used) own = get_shared(p + (long long)lane * kCols * kPartStride + kHeadDim);
+            const float m_all = wave_group_max(row16_max(own.x));
+            const float wt = lane < used ? __builtin_amdgcn_exp2f(own.x - m_all) : 0.f;   // of slice `lane`
             const float den = wave_group_sum(row16_sum(own.y * wt));
-            weight[q][lane] = lane < used ? wt : 0.f;
-            if (lane == 0) weight[q][kDecodeMaxSplit] = den;
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < pairs; i += kThreads) {
-            const int q = i / (kHeadDim / 2), c = 2 * (i % (kHeadDim / 2));
             Float2 num = {0.f, 0.f};
             for (int l = 0; l < used; l += kBatch) {
-                if (l > 0 || i >= kThreads) fetch(i, l);
+                if (l > 0) fetch(l);
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) {
-                    num.x = fmaf(x[u].x, weight[q][l + u], num.x);
-                    num.y = fmaf(x[u].y, weight[q][l + u], num.y);
+                    const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wt), l + u));
+                    num.x = fmaf(x[u].x, w, num.x);
+                    num.y = fmaf(x[u].y, w, num.y);
                 }
             }
-            const float den = weight[q][kDecodeMaxSplit];
             const bool some = sees(token(q)) > 0;
-            store_out(out_row(q) + c, some ? num.x / den : 0.f);
-            store_out(out_row(q) + c + 1, some ? num.y / den : 0.f);
+            store_pair(out_row(q) + 2 * lane, some ? num.x / den : 0.f, some ? num.y / den : 0.f);
         }
     };
     if (used <= 8) merge(std::integral_constant<int, 8>());
