@@ -187,10 +187,12 @@ __device__ __forceinline__ void store_pair(float* p, float x, float y) { *reinte
 // 32 / 8 x 500 6.6 -> 6.4, 16 x 32 / 8 x up to 16384 50.4 -> 49.6.
 // (The scaled 4-bit product, which would take codes as they are, adds up with less than fp32: 1.5e-4 of the sum of
 // magnitudes was measured, and queries would have to be rounded to 8 bits.)
-// What bounds it: long caches the way of their bytes (8 x 32 heads x 8192 keys in 4 bits, 285 MB: 53 us, 5.3 TB/s),
-// many queries the instructions that convert and weigh (2 x 256 queries: 40.7 GFLOP in 62 us, vector and matrix
-// instructions hardly overlap), short caches a
-// chain of latencies (32 / 8 heads x 500 keys: 6.4 us, of which a launch with one load takes 2.5).
+// What bounds it: long caches the way of their bytes (8 x 32 heads x 8192 keys in 4 bits, 285 MB: 51 us, 5.6 TB/s),
+// many queries both pipes (2 x 256 queries x 6000 keys, 40.7 GFLOP: 58 us, 8.9 us for each 1024 keys more, which is
+// 0.95 PFLOP/s where a large library product reaches 1.25; without its exponentials 54.5, without converting codes 53,
+// with all pages from the caches 58), short caches a chain of latencies (32 / 8 heads x 500 keys: 6.0 us, of which a
+// launch with one load takes 2.5).
+
 // Parts of two values: three of them cut off, which is exact, or two rounded.
 template <int PARTS>
 __device__ __forceinline__ void split_pair(float a, float b, unsigned* w)
@@ -274,8 +276,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
         const int q = tile * kCols + col, t = quotient(q, a.by_ratio);
         return out + (hk * ratio + q - t * ratio) * a.os[1] + t * a.os[2];
     };
-    // The slices of a row follow from its own length.  Up to 512 keys are one (8.1 us for 500 in two slices, 6.7 in one),
-    // up to eight slices of 256 are merged in one go (2000 keys 9.6 -> 8.3), beyond that they are longer (8000: 11.9 -> 10.6).
+    // The slices of a row follow from its own length.  Up to 512 keys are one (500 keys: 8.1 us in two, 6.7 in one
+    // then), up to eight slices of 256 are merged in one go (2000 keys 9.6 -> 8.3), beyond that they are longer (8000 keys
+    // 11.9 -> 10.6).
     const int least = held <= 512 ? 512 : held <= 2048 ? 256 : 512;
     const int chunk = max(least, (quotient(held + a.n_split - 1, a.by_split) + kPageRows - 1) / kPageRows * kPageRows);
     const int used = (keys + chunk - 1) / chunk;
@@ -336,7 +339,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
 #pragma unroll
             for (int i = 0; i < kRaw; ++i) k_raw[t][i] = *reinterpret_cast<const u32x4*>(p + key_code_at<BITS>(16 * t + c16, 4 * g4) + 16 * i);
         k_scale = *reinterpret_cast<const unsigned*>(p + page_codes<BITS>() + 4 * lane);
-        asm volatile("" ::: "memory");
+        asm volatile("" ::: "memory");   // (the compiler moves these loads to where they are used)
     };
     auto request_v = [&](int j) {
         const uint8_t* p = vb + (long long)(j / kPageRows) * page_bytes<BITS>();
@@ -347,6 +350,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
         v_scale = *reinterpret_cast<const u32x4*>(p + page_codes<BITS>() + (4 * g4 + (c16 >> 2)) * 16);
         asm volatile("" ::: "memory");
     };
+    // A wave's page; `more`: another one follows, whose codes are requested as soon as this one's are used up.  (As a
+    // condition in the loop the requests made every wait one for all of them: 16 x 32 / 8 x up to 16384 48.4 us, 46.2 so.)
     auto weigh_page = [&](int j, auto more) {
         // scores of the page, a tile of 16 keys after the other
         float s[CT][16];
@@ -571,8 +576,9 @@ CachePlan cache_plan(bool bf16, int B, int Hq, int Hkv, int n, int capacity, int
 {
     const long long cols = (long long)n * (Hq / Hkv), caches = (long long)B * Hkv;
     CachePlan p;
-    // Two column tiles a workgroup halve the conversion of codes, where enough workgroups are left (from half of
-    // that on: 8 x 5 tokens x 32 / 8 heads x 6000 keys 24 -> 21 us, but 4 x 8 x 4000 15.6 -> 18.8).
+    // Two column tiles a workgroup halve the conversion of codes, where a workgroup for each compute unit is left (256
+    // queries of 32 / 8 heads x 8192 keys: 73 us with one, 46 with two; with fewer: 8 x 5 tokens x 32 / 8 x 6000 24 -> 21,
+    // but 4 x 8 x 4000 15.6 -> 18.8).
     p.col_tiles = bf16 && cols > 16 && caches * ((cols + 15) / 16) >= 2 * n_cu ? 2 : 1;
     p.tiles = (int)((cols + 16 * p.col_tiles - 1) / (16 * p.col_tiles));
     // Up to a workgroup of eight waves for each compute unit: of four waves two would leave twice the slices to merge

@@ -2,7 +2,8 @@
 // value against the caller-held anchors, move the threshold, decide, absorb the token into the
 // anchors, append a kept token to the cache of kept keys / values and attend over that cache.
 // Two launches per step: decode_score_kernel (one workgroup per batch row) and the attention over
-// the cache, split over workgroups of which the last to end merges the slices.
+// the cache, split over workgroups of which the last to end merges the slices.  BITS: what the caches hold,
+// 0 rows of the step's type, 4 or 8 quantised ones (cache_format.h), which cache.hip attends to.
 #include <algorithm>
 #include <type_traits>
 
