@@ -594,6 +594,14 @@ CachePlan cache_plan(bool bf16, int B, int Hq, int Hkv, int n, int capacity, int
     return p;
 }
 
+size_t cache_scratch_bytes(int B, int Hq, int Hkv, int n)
+{
+    // (no plan for up to 256 compute units has more than 512 slices, and any only for up to 256 tiles of 16 columns)
+    const long long tiles = (long long)B * Hkv * (((long long)n * (Hq / Hkv) + 15) / 16);
+    if (tiles > 256) return 0;
+    return (size_t)(std::min(512ll, kDecodeMaxSplit * tiles) * 16 * kPartStride + 2 * tiles) * sizeof(float);
+}
+
 hipError_t launch_cache_write(const CacheWriteArgs& in, int dtype, int bits, hipStream_t s)
 {
     CacheWriteArgs a = in;

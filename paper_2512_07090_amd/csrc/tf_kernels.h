@@ -164,6 +164,7 @@ size_t cache_bytes(int bits, long long caches, int capacity);
 // which a (batch row, KV head) has `tiles`, and one of at most `split` slices of its keys; bytes: of workspace.
 struct CachePlan { int col_tiles, waves, tiles, split; size_t bytes; };
 CachePlan cache_plan(bool bf16, int B, int Hq, int Hkv, int n, int capacity, int n_cu);
+size_t cache_scratch_bytes(int B, int Hq, int Hkv, int n);   // enough for every plan of up to 256 compute units
 hipError_t launch_cache_write(const CacheWriteArgs& a, int dtype, int bits, hipStream_t s);
 hipError_t launch_cache_read(const CacheReadArgs& a, int dtype, int bits, hipStream_t s);
 hipError_t launch_cache_attend(const CacheAttendArgs& a, const CachePlan& plan, int dtype, int bits, hipStream_t s);

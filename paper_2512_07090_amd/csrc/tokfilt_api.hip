@@ -675,9 +675,8 @@ size_t tf_cache_workspace_bytes(const tf_params* p)
 {
     const char* why;
     if (check_shape(p, &why) != TF_OK) return 0;
-    // (for 256 compute units and a cache of any capacity)
-    const auto bytes = [&](int n) { return tf::cache_plan(p->dtype != TF_F32, p->batch, p->n_q_heads, p->n_kv_heads, n, INT32_MAX, 256).bytes; };
-    return align256(std::max({bytes(1), bytes(p->seq), (size_t)256}));
+    return align256(std::max({tf::cache_scratch_bytes(p->batch, p->n_q_heads, p->n_kv_heads, 1),
+                              tf::cache_scratch_bytes(p->batch, p->n_q_heads, p->n_kv_heads, p->seq), (size_t)256}));
 }
 
 tf_status tf_cache_write(tf_ctx* ctx, const tf_params* p, const tf_cache* cache, const void* K, const void* V,

@@ -45,6 +45,27 @@ int main()
         const size_t w = tf_cache_workspace_bytes(&x);
         if (w < 256 || w > (64u << 20)) { ++bad; printf("workspace\n"); }
     }
+    // plans of the attention: every column in a tile, slices that a merge can hold, a workspace that is enough
+    for (int dt = 0; dt < 2; ++dt) for (int b : {1, 2, 3, 5, 13, 40, 65, 300}) for (int hkv : {1, 2, 5, 8, 40}) for (int ratio : {1, 3, 4, 8, 17, 71})
+        for (int n : {1, 2, 5, 16, 33, 257}) {
+            const tf_params x = shape(b, hkv * ratio, hkv, n, dt);
+            const size_t w = tf_cache_workspace_bytes(&x);
+            for (int cap : {1, 64, 300, 5000, 1 << 30}) for (int cu = 1; cu <= 256; cu += cu < 8 ? 1 : 31) {
+                const tf::CachePlan q = tf::cache_plan(dt != 0, b, hkv * ratio, hkv, n, cap, cu);
+                const long long tiles = (long long)b * hkv * q.tiles;
+                if (q.bytes > w || q.split < 1 || q.split > 64 || (q.waves != 4 && q.waves != 8) || (q.col_tiles != 1 && !(q.col_tiles == 2 && dt != 0)) ||
+                    16ll * q.col_tiles * q.tiles < n * ratio || 16ll * q.col_tiles * (q.tiles - 1) >= n * ratio || (q.split > 1 && tiles * q.split > 2 * cu)) {
+                    if (bad < 5) printf("plan of %d x %d / %d x %d, capacity %d, %d units\n", b, hkv * ratio, hkv, n, cap, cu);
+                    ++bad;
+                }
+            }
+        }
+    // division by products
+    for (unsigned by = 1; by < 70000; by += by < 300 ? 1 : 977) {
+        const tf::Divisor d = tf::divisor(by);
+        for (long long x : {0ll, (long long)by - 1, (long long)by, 5ll * by + 3, 0x7fffffffll, 0x7fffffffll / by * by, 0x7fffffffll / by * by - 1})
+            if (x >= 0 && x <= 0x7fffffffll && ((((unsigned long long)x * d.mul >> 32) + (unsigned)x) >> d.shift) != (unsigned long long)x / by) { ++bad; printf("%lld / %u\n", x, by); }
+    }
     { tf_params x = p; x.head_dim = 64; if (tf_cache_bytes(&x, 4, 64) || tf_cache_workspace_bytes(&x)) { ++bad; printf("shape\n"); } }
 
     auto write = [&](tf_ctx* cc, const tf_params* pp, const tf_cache* d, const void* k, const void* v, int m) { return tf_cache_write(cc, pp, d, k, v, nullptr, m, nullptr, nullptr); };

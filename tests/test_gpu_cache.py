@@ -322,6 +322,56 @@ def test_calls_on_two_streams_and_from_replayed_graphs(ctx):
     assert torch.equal(c.len, cw.len)
 
 
+def test_rows_beyond_4_gib(ctx):
+    """Caches of more than 2^32 bytes: rows appended at the end of every head's, read back, and attended to among 2^24 - 1
+    others of zeros, whose scores are 0 and whose values add nothing."""
+    Hkv, ratio, cap, n = 4, 2, 1 << 24, 37
+    _say("cache beyond 4 GiB")
+    p = _params("bf16", 1, Hkv * ratio, Hkv, n)
+    assert B.tf_cache_bytes(p, 4, cap) > 1 << 32
+    c = B.QuantCache(p, cap, 4)
+    c.k.zero_()
+    c.v.zero_()
+    c.len.fill_(cap - n)
+    k, v = (_rows((1, Hkv, n, 128), "bf16", s, 0.2) for s in (90, 91))
+    ctx.tf_cache_write(p, c.desc, k, v, None, n, None)
+    ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+    ctx.tf_cache_read(p, c.desc, torch.tensor([cap - n], dtype=torch.int32, device="cuda"), ko, vo)
+    torch.cuda.synchronize()
+    assert c.len.item() == cap and c.overflow.item() == 0
+    kk, vv = (torch.from_numpy(ref.values(*ref.quantise(_f64(x), 4), 4)).cuda() for x in (k, v))
+    assert torch.equal(ko.double(), kk) and torch.equal(vo.double(), vv)
+    one = _params("bf16", 1, Hkv * ratio, Hkv, 1)
+    q = (4 * kk[:, :, -1:].repeat_interleave(ratio, 1)).bfloat16()       # far from all but its own key
+    o = torch.full_like(q, float("nan"))
+    ctx.tf_cache_attend(one, c.desc, q, o, None, torch.empty(B.tf_cache_workspace_bytes(one), dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    for h in range(Hkv * ratio):
+        s = (kk[0, h // ratio] @ q[0, h, 0].double()) * 128 ** -0.5
+        top = s.max().clamp(min=0.0)
+        w = torch.exp(s - top)
+        den = w.sum() + (cap - n) * torch.exp(-top)
+        out, A = (w[:, None] * vv[0, h // ratio]).sum(0) / den, (w[:, None] * vv[0, h // ratio].abs()).sum(0) / den
+        S = (kk[0, h // ratio].abs() @ q[0, h, 0].double().abs()).max() * 128 ** -0.5
+        # the denominator's 2^24 / 64 / 8 / 64 additions a lane of equal terms are exact to 2^-24 each
+        assert ((o[0, h, 0].double() - out).abs() <= (2.0 ** -18 * S + 2.0 ** -14) * A + 2.0 ** -8 * out.abs()).all(), h
+
+
+def test_the_same_call_gives_the_same_bits(ctx):
+    Bn, Hq, Hkv, cap = 3, 16, 4, 5000
+    _say("cache attend repeated")
+    for n in (1, 6):
+        p = _params("bf16", Bn, Hq, Hkv, n)
+        c, _, _ = _quant_cache(p, "bf16", 4, Bn, Hkv, [5000, 4321, 700], cap, 95)
+        q = _rows((Bn, Hq, n, 128), "bf16", 96)
+        ws = torch.empty(B.tf_cache_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+        outs = [torch.empty_like(q) for _ in range(12)]
+        for o in outs:
+            ctx.tf_cache_attend(p, c.desc, q, o, None, ws)
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, outs[0]) for o in outs)
+
+
 def test_two_graphs_share_a_workspace(ctx):
     """Two layers captured apart, with other lengths and other numbers of slices, replayed in turn over one workspace."""
     Bn, Hq, Hkv, cap = 2, 8, 2, 3000
