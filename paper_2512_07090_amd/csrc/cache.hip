@@ -530,38 +530,35 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
     if (drawn != used - 1) return;
     // (a replayed graph calls by the same number again)
     if (threadIdx.x == 0) __hip_atomic_store(ticket, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    auto merge = [&](auto batch) {
-        constexpr int kBatch = decltype(batch)::value;
-        for (int q = wave; q < cols; q += WAVES) {
-            const float* const p = part0 + q * kPartStride;
-            // (the first slices' numerators are requested before their weights are known)
-            Float2 x[kBatch];
-            auto fetch = [&](int l) {
+    // (eight slices at a time: 32 at once 17.3 us for 8 tokens x 32 / 8 heads x 16000 keys, 14.8 so; several waves a column: even)
+    constexpr int kBatch = 8;
+    for (int q = wave; q < cols; q += WAVES) {
+        const float* const p = part0 + q * kPartStride;
+        // (the first slices' numerators are requested before their weights are known)
+        Float2 x[kBatch];
+        auto fetch = [&](int l) {
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u) x[u] = get_shared(p + (long long)min(l + u, used - 1) * kCols * kPartStride + 2 * lane);
-            };
-            fetch(0);
-            Float2 own = {kLowest, 0.f};
-            if (lane < used) own = get_shared(p + (long long)lane * kCols * kPartStride + kHeadDim);
-            const float m_all = wave_group_max(row16_max(own.x));
-            const float wt = lane < used ? __builtin_amdgcn_exp2f(own.x - m_all) : 0.f;   // of slice `lane`
-            const float den = wave_group_sum(row16_sum(own.y * wt));
-            Float2 num = {0.f, 0.f};
-            for (int l = 0; l < used; l += kBatch) {
-                if (l > 0) fetch(l);
+            for (int u = 0; u < kBatch; ++u) x[u] = get_shared(p + (long long)min(l + u, used - 1) * kCols * kPartStride + 2 * lane);
+        };
+        fetch(0);
+        Float2 own = {kLowest, 0.f};
+        if (lane < used) own = get_shared(p + (long long)lane * kCols * kPartStride + kHeadDim);
+        const float m_all = wave_group_max(row16_max(own.x));
+        const float wt = lane < used ? __builtin_amdgcn_exp2f(own.x - m_all) : 0.f;   // of slice `lane`
+        const float den = wave_group_sum(row16_sum(own.y * wt));
+        Float2 num = {0.f, 0.f};
+        for (int l = 0; l < used; l += kBatch) {
+            if (l > 0) fetch(l);
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u) {
-                    const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wt), l + u));
-                    num.x = fmaf(x[u].x, w, num.x);
-                    num.y = fmaf(x[u].y, w, num.y);
-                }
+            for (int u = 0; u < kBatch; ++u) {
+                const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wt), l + u));
+                num.x = fmaf(x[u].x, w, num.x);
+                num.y = fmaf(x[u].y, w, num.y);
             }
-            const bool some = sees(token(q)) > 0;
-            store_pair(out_row(q) + 2 * lane, some ? num.x / den : 0.f, some ? num.y / den : 0.f);
         }
-    };
-    if (used <= 8) merge(std::integral_constant<int, 8>());
-    else merge(std::integral_constant<int, 32>());
+        const bool some = sees(token(q)) > 0;
+        store_pair(out_row(q) + 2 * lane, some ? num.x / den : 0.f, some ? num.y / den : 0.f);
+    }
 }
 
 }  // namespace
