@@ -276,10 +276,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
         const int q = tile * kCols + col, t = quotient(q, a.by_ratio);
         return out + (hk * ratio + q - t * ratio) * a.os[1] + t * a.os[2];
     };
-    // The slices of a row follow from its own length.  Up to 512 keys are one (500 keys: 8.1 us in two, 6.7 in one
-    // then), up to eight slices of 256 are merged in one go (2000 keys 9.6 -> 8.3), beyond that they are longer (8000 keys
-    // 11.9 -> 10.6).
-    const int least = held <= 512 ? 512 : held <= 2048 ? 256 : 512;
+    // The slices of a row follow from its own length.  Up to 512 keys are one (500 keys: 8.1 us in two, 6.7 in one then),
+    // and what is left to the others is at most 16 of them, whose merge costs less than 32 compute units bring: of 256,
+    // 512, 1024 keys 1 x 32 / 8 heads x 4000 keys 8.1, 8.1, 9.1 us; 8000 10.7, 9.2, 9.3; 16000 12.4, 12.4, 11.1; 8 / 1 heads
+    // x 4000 7.7, 8.4, 9.4.
+    const int least = held <= 512 ? 512 : held <= 4096 ? 256 : held <= 8192 ? 512 : 1024;
     const int chunk = max(least, (quotient(held + a.n_split - 1, a.by_split) + kPageRows - 1) / kPageRows * kPageRows);
     const int used = (keys + chunk - 1) / chunk;
     if (sp >= used) {

@@ -215,6 +215,25 @@ def test_attend_strided_scaled_and_sharp(ctx):
     assert torch.isnan(o.as_strided((Bn, n, Hq, 8), (n * Hq * 136, Hq * 136, 136, 1), o.storage_offset() + 128)).all()
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_attend_on_both_sides_of_the_slices_borders(ctx, dt):
+    """Lengths at which a row's slices change in size, and their number."""
+    lens, cap = [513, 4097, 8193, 1025, 2049], 8200
+    Bn, Hq, Hkv = len(lens), 4, 1
+    _say("cache attend slices %s" % dt)
+    p = _params(dt, Bn, Hq, Hkv, 1)
+    c, k, v = _quant_cache(p, dt, 4, Bn, Hkv, lens, cap, 36)
+    q = _rows((Bn, Hq, 1, 128), dt, 37, 0.2)
+    ws = torch.full((B.tf_cache_workspace_bytes(p),), 0xFF, dtype=torch.uint8, device="cuda")
+    for less in (0, 1, 2, 65, 513):
+        cur = [n - less for n in lens]
+        c.len.copy_(torch.tensor(cur, dtype=torch.int32))
+        o = torch.full_like(q, float("nan"))
+        ctx.tf_cache_attend(p, c.desc, q, o, None, ws)
+        torch.cuda.synchronize()
+        _check_attention(o, ref.attend(q.double(), k, v, cur, [1] * Bn, 128 ** -0.5), dt)
+
+
 @pytest.mark.parametrize("case", [("bf16", 2, 8, 2, 3), ("bf16", 2, 8, 2, 12), ("f32", 2, 4, 2, 5), ("bf16", 20, 16, 8, 40)])
 def test_padding_may_hold_anything(ctx, case):
     """Queries from count on, and rows of the cache behind its length, are NaN and infinities: no trace of them."""
