@@ -188,9 +188,9 @@ __device__ __forceinline__ void store_pair(float* p, float x, float y) { *reinte
 // (The scaled 4-bit product, which would take codes as they are, adds up with less than fp32: 1.5e-4 of the sum of
 // magnitudes was measured, and queries would have to be rounded to 8 bits.)
 // What bounds it: long caches the way of their bytes (8 x 32 heads x 8192 keys in 4 bits, 285 MB: 51 us, 5.6 TB/s),
-// many queries both pipes (2 x 256 queries x 6000 keys, 40.7 GFLOP: 58 us, 8.9 us for each 1024 keys more, which is
+// many queries both pipes (2 x 256 queries x 6000 keys, 40.7 GFLOP: 57 us, 8.9 us for each 1024 keys more, which is
 // 0.95 PFLOP/s where a large library product reaches 1.25; without its exponentials 54.5, without converting codes 53,
-// with all pages from the caches 58), short caches a chain of latencies (32 / 8 heads x 500 keys: 6.0 us, of which a
+// with all pages from the caches 58), short caches a chain of latencies (32 / 8 heads x 500 keys: 5.9 us, of which a
 // launch with one load takes 2.5).
 
 // Parts of two values: three of them cut off, which is exact, or two rounded.
@@ -575,8 +575,8 @@ CachePlan cache_plan(bool bf16, int B, int Hq, int Hkv, int n, int capacity, int
     const long long cols = (long long)n * (Hq / Hkv), caches = (long long)B * Hkv;
     CachePlan p;
     // Two column tiles a workgroup halve the conversion of codes, where a workgroup for each compute unit is left (256
-    // queries of 32 / 8 heads x 8192 keys: 73 us with one, 46 with two; with fewer: 8 x 5 tokens x 32 / 8 x 6000 24 -> 21,
-    // but 4 x 8 x 4000 15.6 -> 18.8).
+    // queries of 32 / 8 heads x 8192 keys: 73 us with one, 46 with two; with fewer: 8 x 5 tokens x 32 / 8 x 6000 20 -> 17,
+    // but 4 x 8 x 4000 13.0 -> 15.1, 8 x 16000 14.6 -> 18.0, 128 x 2000 14.5 -> 16.2).
     p.col_tiles = bf16 && cols > 16 && caches * ((cols + 15) / 16) >= 2 * n_cu ? 2 : 1;
     p.tiles = (int)((cols + 16 * p.col_tiles - 1) / (16 * p.col_tiles));
     // Up to a workgroup of eight waves for each compute unit: of four waves two would leave twice the slices to merge

@@ -3,7 +3,7 @@
 // It lives on memory bandwidth: every row is read once and written once, 16 lanes a row, eight columns a lane.
 // All heads of a token turn by the same angles; a workgroup takes 16 heads of four tokens, makes the four
 // tables meanwhile its 64 rows are on their way (a wave a token, a lane a frequency), and each lane turns four
-// rows of one token.  8 x 4096 tokens x 32 + 32 heads, bf16, 1.07 GB: 188 us, 5.7 TB/s (a copy: 4.8); with all
+// rows of one token.  8 x 4096 tokens x 32 + 32 heads, bf16, 1.07 GB: 190 us, 5.6 TB/s (a copy: 4.8); with all
 // heads of a token in one workgroup, row after row, 268.  One token x 32 + 8 heads: 2.8 us against 11.
 #include "decode_device.h"
 #include "tf_kernels.h"
