@@ -327,7 +327,9 @@ tf_status tf_norm_rotate(tf_ctx *ctx, const tf_params *p, const tf_rotary *r, co
 /* A cache in 4 or 8 bits.  A row of 128 columns is held as four blocks of 32, each of them codes and one
  * scale s = 2^(E - 127), E in a byte: s is the smallest power of two, at least 2^-126, with max|x| <= 6 s
  * (TF_CACHE_FP4) or 448 s (TF_CACHE_FP8), and a code is x / s rounded to nearest, ties to even, as e2m1
- * (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) or e4m3.  Magnitudes must be below 2^126.
+ * (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) or e4m3.  Magnitudes must be below 2^126.  A block that
+ * holds a NaN or an infinity has E = 255: all of it reads back as NaN, and a query that sees it gets NaN (as
+ * may the call's other queries of that batch row and KV head; no others do).
  * Rows lie in pages of 64 for each (batch row, KV head): [batch][n_kv_heads][ceil(capacity / 64)][page],
  * a page being 64 rows of codes (C = 64 or 128 bytes a row) and then 256 scale bytes.  With r the row in
  * its page, c its column, e = C / 16 the bytes of eight columns:

@@ -3,7 +3,8 @@
 // A row of 128 columns is four blocks of 32, each with one scale s = 2^(E - 127), E in a byte: the smallest
 // power of two, E >= 1, with max|x| <= M s (M = 6, the largest e2m1 value, or 448, the largest e4m3 value).
 // A code is x / s rounded to nearest even.  Dividing by a power of two is exact, so codes do not depend on
-// how they are computed, nothing saturates, and both types convert in the hardware.
+// how they are computed, nothing saturates, and both types convert in the hardware.  A block that holds a NaN or
+// an infinity has E = 255, of which the hardware's conversions make a NaN whatever the code.
 //
 // A page holds 64 rows of one head: their codes, then 256 scale bytes.  Keys lie as rows (a lane of the
 // attention reads one block of one key), their scales as [block][row % 16][row / 16], so that one dword is the
@@ -30,12 +31,14 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 
+// the larger magnitude, a NaN if either is one (fmaxf passes over it, and a 4-bit code cannot hold it)
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 // exponent byte of a block whose largest magnitude is `top`: mantissas up to that of M keep the exponent
 template <int BITS>
 __device__ __forceinline__ int block_exponent(float top)
 {
     const int e = (int)((__float_as_uint(top) + (BITS == 4 ? 0x3fffffu : 0x1fffffu)) >> 23) - (BITS == 4 ? 2 : 8);
-    return max(e, 1);
+    return top < INFINITY ? max(e, 1) : 255;
 }
 __device__ __forceinline__ float exponent_scale(int e) { return __uint_as_float((unsigned)e << 23); }
 
@@ -127,9 +130,9 @@ __device__ __forceinline__ void store_row8(uint8_t* page, int row, int c, const 
 {
     float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
-    top = fmaxf(top, dpp_mov<0xB1>(top));   // the four lanes of a block
-    top = fmaxf(top, dpp_mov<0x4E>(top));
+    for (int i = 0; i < 8; ++i) top = larger(top, fabsf(x[i]));
+    top = larger(top, dpp_mov<0xB1>(top));   // the four lanes of a block
+    top = larger(top, dpp_mov<0x4E>(top));
     const int e = block_exponent<BITS>(top);
     unsigned w[BITS / 4];
     codes_of8<BITS>(x, exponent_scale(e), w);

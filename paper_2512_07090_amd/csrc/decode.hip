@@ -219,7 +219,12 @@ __device__ __forceinline__ void score_row(
             for (int i = 0; i < 4; ++i) {
                 float x[2];
                 unpack2(pr == grp ? first[i] : *reinterpret_cast<const Pair*>(src + 32 * i), x);
-                const int e = block_exponent<BITS>(row16_max(fmaxf(fabsf(x[0]), fabsf(x[1]))));
+                float top = larger(fabsf(x[0]), fabsf(x[1]));   // of the 16 lanes
+                top = larger(top, dpp_mov<0xB1>(top));
+                top = larger(top, dpp_mov<0x4E>(top));
+                top = larger(top, dpp_mov<0x141>(top));
+                top = larger(top, dpp_mov<0x140>(top));
+                const int e = block_exponent<BITS>(top);
                 const unsigned code = codes_of2<BITS>(x[0], x[1], exponent_scale(e));
                 const int c = 4 * i + (l16 >> 2);   // eight columns 8 c, of which this lane has the pair l16 % 4
                 uint8_t* const at = page + (w ? value_code_at<BITS>(row, c) : key_code_at<BITS>(row, c)) + (l16 & 3) * (BITS / 4);
