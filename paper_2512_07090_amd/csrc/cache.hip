@@ -600,15 +600,21 @@ size_t cache_scratch_bytes(int B, int Hq, int Hkv, int n)
     return (size_t)(std::min(512ll, kDecodeMaxSplit * tiles) * 16 * kPartStride + 2 * tiles) * sizeof(float);
 }
 
+static int pages_touched(int rows) { return (rows + kPageRows - 2) / kPageRows + 1; }   // by `rows` rows behind any others
+
+bool cache_write_few(int Hkv, int m) { return 2ll * Hkv * m <= kAppendRows; }
+long long cache_write_workgroups(int B, int Hkv, int m) { return cache_write_few(Hkv, m) ? B : 2ll * pages_touched(m) * B * Hkv; }
+long long cache_read_workgroups(int B, int Hkv, int n) { return 2ll * pages_touched(n) * B * Hkv; }
+
 hipError_t launch_cache_write(const CacheWriteArgs& in, int dtype, int bits, hipStream_t s)
 {
     CacheWriteArgs a = in;
-    a.pages = (a.m + kPageRows - 2) / kPageRows + 1;   // of a.m rows behind any others
-    const bool few = 2ll * a.Hkv * a.m <= kAppendRows;
-    const unsigned grid = (unsigned)(2ll * a.pages * a.B * a.Hkv);
+    a.pages = pages_touched(a.m);
+    const bool few = cache_write_few(a.Hkv, a.m);
+    const unsigned grid = (unsigned)cache_write_workgroups(a.B, a.Hkv, a.m);
 #define TF_CACHE_WRITE(T, BITS)                                                                   \
     do {                                                                                          \
-        if (few) cache_append_kernel<T, BITS><<<dim3((unsigned)a.B), dim3((unsigned)append_threads), 0, s>>>(a); \
+        if (few) cache_append_kernel<T, BITS><<<dim3(grid), dim3((unsigned)append_threads), 0, s>>>(a); \
         else cache_write_kernel<T, BITS><<<dim3(grid), dim3(256), 0, s>>>(a);                     \
     } while (0)
     const int append_threads = std::min(1024, (2 * a.Hkv * (few ? a.m : 1) * 16 + 63) / 64 * 64);
@@ -629,8 +635,8 @@ hipError_t launch_cache_write(const CacheWriteArgs& in, int dtype, int bits, hip
 hipError_t launch_cache_read(const CacheReadArgs& in, int dtype, int bits, hipStream_t s)
 {
     CacheReadArgs a = in;
-    a.pages = (a.n + kPageRows - 2) / kPageRows + 1;
-    const unsigned grid = (unsigned)(2ll * a.pages * a.B * a.Hkv);
+    a.pages = pages_touched(a.n);
+    const unsigned grid = (unsigned)cache_read_workgroups(a.B, a.Hkv, a.n);
     // (results that would push everything out of the 256 MB cache behind the L2s; smaller ones are what is used next)
     const bool stream = 2ll * (dtype == 0 ? 4 : 2) * kHeadDim * a.B * a.Hkv * a.n > (256ll << 20);
 #define TF_CACHE_READ(T, BITS)                                                                    \

@@ -114,19 +114,26 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(const NormRotateArgs a
 
 }  // namespace
 
+// Where four tokens a workgroup leave no more than two on a compute unit, one each: latency counts there
+// (32 + 8 heads, 16 / 200 / 1000 / 2048 tokens: 4.7, 4.9, 8.5, 12.5 us by fours, 3.4, 4.2, 9.0, 13.8 one by one).
+static bool one_by_one(const NormRotateArgs& a) { return a.n < 4 || (long long)a.B * a.n * a.parts <= 4 * 512; }
+
+long long norm_rotate_workgroups(NormRotateArgs& a)
+{
+    a.parts_q = a.Q ? (a.Hq + 15) / 16 : 0;
+    a.parts = a.parts_q + (a.K ? (a.Hkv + 15) / 16 : 0);
+    return (long long)a.parts * a.B * (one_by_one(a) ? a.n : (a.n + 3) / 4);
+}
+
 hipError_t launch_norm_rotate(const NormRotateArgs& in, int dtype, hipStream_t s)
 {
     NormRotateArgs a = in;
-    a.parts_q = a.Q ? (a.Hq + 15) / 16 : 0;
-    a.parts = a.parts_q + (a.K ? (a.Hkv + 15) / 16 : 0);
+    const unsigned grid = (unsigned)norm_rotate_workgroups(a);
+    const bool few = one_by_one(a);
     const long long rows = (long long)a.B * a.n;
-    // Where four tokens a workgroup leave no more than two on a compute unit, one each: latency counts there
-    // (32 + 8 heads, 16 / 200 / 1000 / 2048 tokens: 4.7, 4.9, 8.5, 12.5 us by fours, 3.4, 4.2, 9.0, 13.8 one by one).
-    const bool few = a.n < 4 || rows * a.parts <= 4 * 512;
     // Results that would push everything out of the 256 MB cache behind the L2s go past it (the case above
     // 206 us without); smaller ones are what the next call reads.
     const bool stream = (dtype == 0 ? 8 : 4) * rows * kHeadDim * ((a.Q ? a.Hq : 0) + (a.K ? a.Hkv : 0)) > (256ll << 20);
-    const unsigned grid = (unsigned)a.parts * a.B * (unsigned)(few ? a.n : (a.n + 3) / 4);
 #define TF_NORM_ROTATE(T)                                                                          \
     do {                                                                                          \
         if (few) norm_rotate_kernel<T, 1, false><<<dim3(grid), dim3(256), 0, s>>>(a);             \

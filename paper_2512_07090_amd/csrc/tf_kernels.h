@@ -119,6 +119,8 @@ struct NormRotateArgs {
     int B, Hq, Hkv, n, parts_q, parts;              // parts: workgroups for a token's heads
     long long qs[3], kvs[3], os[3];
 };
+// Workgroups for 16 heads of one to four tokens of a tensor, of 256 threads (parts and parts_q are set by it).
+long long norm_rotate_workgroups(NormRotateArgs& a);
 hipError_t launch_norm_rotate(const NormRotateArgs& a, int dtype, hipStream_t s);
 
 // ---- a cache in 4 or 8 bits (cache_format.h) ------------------------------------------------------
@@ -160,6 +162,10 @@ struct CacheAttendArgs {
     long long qs[3], os[3];
 };
 size_t cache_bytes(int bits, long long caches, int capacity);
+// Workgroups that write m rows or read n back, for up to 1024 threads where few rows are written and 256 else.
+bool cache_write_few(int Hkv, int m);
+long long cache_write_workgroups(int B, int Hkv, int m);
+long long cache_read_workgroups(int B, int Hkv, int n);
 // How the attention is cut up: a workgroup of `waves` takes col_tiles x 16 columns (queries x heads of a KV head), of
 // which a (batch row, KV head) has `tiles`, and one of at most `split` slices of its keys; bytes: of workspace.
 struct CachePlan { int col_tiles, waves, tiles, split; size_t bytes; };

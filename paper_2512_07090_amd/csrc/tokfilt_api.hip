@@ -269,11 +269,8 @@ int cache_pages(int32_t capacity) { return (int)(((int64_t)capacity + 63) / 64);
 // an output whose rows share memory
 bool folded(const int64_t* stride, int batch, int heads) { return (batch > 1 && stride[0] == 0) || (heads > 1 && stride[1] == 0); }
 
-// workgroups of the calls that walk pages: one each for a page of a tensor's (batch row, KV head)
-bool too_many_pages(const tf_params* p, int rows)
-{
-    return 2 * ((int64_t)rows / 64 + 2) * p->batch * p->n_kv_heads >= ((int64_t)1 << 31);
-}
+// the runtime launches fewer than 2^32 threads at a time
+bool too_many_threads(int64_t workgroups, int threads) { return workgroups >= ((int64_t)1 << 32) / threads; }
 
 }  // namespace
 
@@ -650,17 +647,15 @@ tf_status tf_norm_rotate(tf_ctx* ctx, const tf_params* p, const tf_rotary* r, co
                 return fail(ctx, TF_ERR_INVALID_ARG, "in place the strides of Q and of its output must be equal");
     if ((Q && folded(p->o_stride, p->batch, p->n_q_heads)) || (K && folded(p->kv_stride, p->batch, p->n_kv_heads)))
         return fail(ctx, TF_ERR_INVALID_ARG, "an output must not have a stride of 0");
-    // a workgroup for 16 heads of one to four tokens
-    if ((int64_t)p->batch * p->seq * ((p->n_q_heads + 15) / 16 + (p->n_kv_heads + 15) / 16) >= ((int64_t)1 << 31))
-        return fail(ctx, TF_ERR_UNSUPPORTED, "too many rows for one call");
-    st = use_device(ctx);
-    if (st != TF_OK) return st;
     tf::NormRotateArgs a;
     a.Q = Q; a.K = K; a.Q_out = Q_out; a.K_out = K_out;
     a.q_weight = r->q_weight; a.k_weight = r->k_weight; a.freq = r->freq; a.positions = r->positions; a.start = r->start;
     a.eps = r->eps; a.rot_dim = r->rot_dim; a.interleaved = r->interleaved;
     a.B = p->batch; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.n = p->seq;
     for (int i = 0; i < 3; ++i) { a.qs[i] = p->q_stride[i]; a.kvs[i] = p->kv_stride[i]; a.os[i] = p->o_stride[i]; }
+    if (too_many_threads(tf::norm_rotate_workgroups(a), 256)) return fail(ctx, TF_ERR_UNSUPPORTED, "too many rows for one call");
+    st = use_device(ctx);
+    if (st != TF_OK) return st;
     return dev(ctx, tf::launch_norm_rotate(a, p->dtype, (hipStream_t)stream), "norm and rotation launch");
 }
 
@@ -687,7 +682,8 @@ tf_status tf_cache_write(tf_ctx* ctx, const tf_params* p, const tf_cache* cache,
     if (!K || !V) return fail(ctx, TF_ERR_INVALID_ARG, "K and V must not be NULL");
     if (misaligned(K) || misaligned(V)) return fail(ctx, TF_ERR_INVALID_ARG, "K and V must be 16-byte aligned");
     if (m < 1 || m > p->seq) return fail(ctx, TF_ERR_INVALID_ARG, "m must be in [1, seq]");
-    if (too_many_pages(p, m)) return fail(ctx, TF_ERR_UNSUPPORTED, "too many rows for one call");
+    if (too_many_threads(tf::cache_write_workgroups(p->batch, p->n_kv_heads, m), tf::cache_write_few(p->n_kv_heads, m) ? 1024 : 256))
+        return fail(ctx, TF_ERR_UNSUPPORTED, "too many rows for one call");
     st = use_device(ctx);
     if (st != TF_OK) return st;
     tf::CacheWriteArgs a;
@@ -707,7 +703,7 @@ tf_status tf_cache_read(tf_ctx* ctx, const tf_params* p, const tf_cache* cache, 
     if (!K || !V) return fail(ctx, TF_ERR_INVALID_ARG, "K and V must not be NULL");
     if (misaligned(K) || misaligned(V)) return fail(ctx, TF_ERR_INVALID_ARG, "K and V must be 16-byte aligned");
     if (folded(p->kv_stride, p->batch, p->n_kv_heads)) return fail(ctx, TF_ERR_INVALID_ARG, "an output must not have a stride of 0");
-    if (too_many_pages(p, p->seq)) return fail(ctx, TF_ERR_UNSUPPORTED, "too many rows for one call");
+    if (too_many_threads(tf::cache_read_workgroups(p->batch, p->n_kv_heads, p->seq), 256)) return fail(ctx, TF_ERR_UNSUPPORTED, "too many rows for one call");
     st = use_device(ctx);
     if (st != TF_OK) return st;
     tf::CacheReadArgs a;
@@ -731,6 +727,8 @@ tf_status tf_cache_attend(tf_ctx* ctx, const tf_params* p, const tf_cache* cache
     if ((int64_t)p->batch * p->n_kv_heads * (((int64_t)p->seq * (p->n_q_heads / p->n_kv_heads) + 15) / 16) >= ((int64_t)1 << 25))
         return fail(ctx, TF_ERR_UNSUPPORTED, "too many queries for one call");
     const tf::CachePlan plan = tf::cache_plan(p->dtype != TF_F32, p->batch, p->n_q_heads, p->n_kv_heads, p->seq, cache->capacity, std::min(ctx->n_cu, 256));
+    if (too_many_threads((int64_t)p->batch * p->n_kv_heads * plan.tiles * plan.split, 64 * plan.waves))
+        return fail(ctx, TF_ERR_UNSUPPORTED, "too many queries for one call");
     if (ws_bytes < plan.bytes)
         return fail(ctx, TF_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, plan.bytes);
     st = use_device(ctx);
