@@ -81,13 +81,13 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(const NormRotateArgs a
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int col = 8 * l16 + i;
-        const float2 r = col >= a.rot_dim ? make_float2(1.f, 0.f)
-                       : turn[tok][a.interleaved ? col / 2 : col < half ? col : col - half];
+        const float2 r = turn[tok][col >= a.rot_dim ? 0 : a.interleaved ? col / 2 : col < half ? col : col - half];
         const bool second = a.interleaved ? col & 1 : col >= half;
         cs[i] = r.x;
         sn[i] = second ? r.y : -r.y;
     }
-    const int hop = half / 8, mate = 8 * l16 >= a.rot_dim ? l16 : l16 < hop ? l16 + hop : l16 - hop;
+    const bool turned = 8 * l16 < a.rot_dim;   // (rot_dim is a multiple of 16: all of a lane's columns or none)
+    const int hop = half / 8, mate = !turned ? l16 : l16 < hop ? l16 + hop : l16 - hop;
     const int from = (lane & 48) + mate;
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
@@ -108,6 +108,9 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(const NormRotateArgs a
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = fmaf(x[u][i], cs[i], __shfl(x[u][i], from) * sn[i]);
         }
+        // (no arithmetic for what is passed on: by cos 1 and sin 0 an infinity would become a NaN)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = turned ? y[i] : x[u][i];
         if (h < heads && t0 + tok < a.n) store_row<STREAM>(dst + h * o_h + t * o_t, y);
     }
 }
