@@ -12,6 +12,7 @@ namespace tf {
 namespace {
 
 constexpr int kPartStride = kDecodePartFloats;
+constexpr float kNoKey = -3.0e38f;   // the maximum of no scores: below all of them, and finite, so differences of two are 0
 
 // STREAM: past the caches
 template <bool STREAM>
@@ -328,7 +329,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
     for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[ct][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        mx[ct] = kLowest; sum[ct] = 0.f;
+        mx[ct] = kNoKey; sum[ct] = 0.f;
         total[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     u32x4 k_raw[4][kRaw], v_raw[4][kRaw], v_scale;
@@ -355,7 +356,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
     // condition in the loop the requests made every wait one for all of them: 16 x 32 / 8 x up to 16384 48.4 us, 46.2 so.)
     auto weigh_page = [&](int j, auto more) {
         // scores of the page, a tile of 16 keys after the other
-        float s[CT][16];
+        float s[CT][16], factor[CT];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const float scale = exponent_scale((k_scale >> (8 * t)) & 0xff);
@@ -408,6 +409,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
 #pragma unroll
                 for (int i = 0; i < 8; ++i) acc[ct][i] *= down;
             }
+            // Weights are exp2(s scale - mx) in one rounding.  Beyond 2^24 what the maximum lost in its own could overflow an
+            // exponent, so scores are rounded like it there: equal ones have equal weights, whatever their size.
+            factor[ct] = a.scale_log2e;
+            const bool far = fabsf(mx[ct]) > 0x1p24f && mx[ct] > kNoKey;
+            if (__any(far)) {
+                const float first = far ? a.scale_log2e : 1.f;   // (a column's own: its neighbours keep their rounding)
+                factor[ct] = far ? 1.f : a.scale_log2e;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[ct][i] *= first;
+            }
         }
         // keys behind the last (of the wave's last page): whatever lies there, their weights are zero and so are their values
         const bool clear = !more && j + kPageRows > hi;
@@ -418,8 +429,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    const float p0 = __builtin_amdgcn_exp2f(fmaf(s[ct][8 * h + e], a.scale_log2e, -mx[ct]));
-                    const float p1 = __builtin_amdgcn_exp2f(fmaf(s[ct][8 * h + e + 1], a.scale_log2e, -mx[ct]));
+                    const float p0 = __builtin_amdgcn_exp2f(fmaf(s[ct][8 * h + e], factor[ct], -mx[ct]));
+                    const float p1 = __builtin_amdgcn_exp2f(fmaf(s[ct][8 * h + e + 1], factor[ct], -mx[ct]));
                     if constexpr (kWholeSum) sum[ct] += p0 + p1;
                     unsigned w[kP];
                     if constexpr (PAIRED) {
@@ -499,7 +510,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
     // From here on a wave takes whole columns, a lane two neighbouring values.
     float* const part0 = a.part + ((long long)bh * a.tiles + tile) * a.n_split * kCols * kPartStride;   // [slice][column]
     for (int q = wave; q < cols; q += WAVES) {
-        float m_all = kLowest, den = 0.f;
+        float m_all = kNoKey, den = 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) m_all = fmaxf(m_all, stat[w][q][0]);
         Float2 v = {0.f, 0.f};
@@ -542,7 +553,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
             for (int u = 0; u < kBatch; ++u) x[u] = get_shared(p + (long long)min(l + u, used - 1) * kCols * kPartStride + 2 * lane);
         };
         fetch(0);
-        Float2 own = {kLowest, 0.f};
+        Float2 own = {kNoKey, 0.f};
         if (lane < used) own = get_shared(p + (long long)lane * kCols * kPartStride + kHeadDim);
         const float m_all = wave_group_max(row16_max(own.x));
         const float wt = lane < used ? __builtin_amdgcn_exp2f(own.x - m_all) : 0.f;   // of slice `lane`
