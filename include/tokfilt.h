@@ -362,8 +362,8 @@ tf_status tf_cache_write(tf_ctx *ctx, const tf_params *p, const tf_cache *cache,
                          void *stream);
 
 /* Reads rows start[b] .. start[b] + seq - 1 (start NULL: from 0; negative: 0) back into rows 0 .. of K and
- * V (p->kv_stride), exactly what the codes stand for.  Rows that the cache does not hold are left as they
- * were. */
+ * V (p->kv_stride), exactly what the codes stand for (in TF_BF16 cut off below 2^-133, which only codes of
+ * TF_F32 rows reach).  Rows that the cache does not hold are left as they were. */
 tf_status tf_cache_read(tf_ctx *ctx, const tf_params *p, const tf_cache *cache, const int32_t *start,
                         void *K, void *V, void *stream);
 
@@ -373,9 +373,9 @@ tf_status tf_cache_read(tf_ctx *ctx, const tf_params *p, const tf_cache *cache, 
  *   Q  in  p->q_stride, O  out  p->o_stride (must not overlap), count  DEVICE [batch], 0 .. seq, or NULL
  * Arithmetic: what the codes stand for enters exactly; fp32 softmax and accumulation; queries as they
  * are.  Weights are fp32 for TF_F32; for TF_BF16, whose output is rounded to bf16, they are held to 2^-16 of
- * themselves, or, in calls of so many queries that the arithmetic is what they wait for (batch * n_kv_heads
- * * ceil(seq * n_q_heads / n_kv_heads / 16) of two per compute unit or more), rounded to bf16 once, as in
- * tf_attend, and summed as rounded.
+ * themselves, or, in calls of so many queries that the arithmetic is what they wait for, rounded to bf16 once,
+ * as in tf_attend, and summed as rounded.  These are calls in which a KV head has c = seq * n_q_heads /
+ * n_kv_heads > 16 columns and batch * n_kv_heads * ceil(c / 16) is at least two per compute unit.
  * A row's results, rounding included, follow from its own queries, keys, len and count, `p` and
  * cache->capacity alone. */
 tf_status tf_cache_attend(tf_ctx *ctx, const tf_params *p, const tf_cache *cache, const void *Q, void *O,
