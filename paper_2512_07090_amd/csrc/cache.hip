@@ -24,7 +24,7 @@ __device__ __forceinline__ void put16(void* p, u32x4 v)
 template <bool STREAM>
 __device__ __forceinline__ void store8(uint16_t* p, const float* x)
 {
-    u32x4 r;   // (what a code stands for is exact in bf16)
+    u32x4 r;   // (what a code stands for is exact in bf16 down to 2^-133)
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_perm(__float_as_uint(x[2 * i + 1]), __float_as_uint(x[2 * i]), 0x07060302u);
     put16<STREAM>(p, r);
@@ -278,9 +278,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
         return out + (hk * ratio + q - t * ratio) * a.os[1] + t * a.os[2];
     };
     // The slices of a row follow from its own length.  Up to 512 keys are one (500 keys: 8.1 us in two, 6.7 in one then),
-    // and what is left to the others is at most 16 of them, whose merge costs less than 32 compute units bring: of 256,
-    // 512, 1024 keys 1 x 32 / 8 heads x 4000 keys 8.1, 8.1, 9.1 us; 8000 10.7, 9.2, 9.3; 16000 12.4, 12.4, 11.1; 8 / 1 heads
-    // x 4000 7.7, 8.4, 9.4.
+    // rows of up to 16384 at most 16, whose merge costs less than 32 compute units bring, and longer ones up to n_split
+    // (kDecodeMaxSplit at most) of 1024 keys or more: of 256, 512, 1024 keys 1 x 32 / 8 heads x 4000 keys 8.1, 8.1, 9.1 us;
+    // 8000 10.7, 9.2, 9.3; 16000 12.4, 12.4, 11.1; 8 / 1 heads x 4000 7.7, 8.4, 9.4.
     const int least = held <= 512 ? 512 : held <= 4096 ? 256 : held <= 8192 ? 512 : 1024;
     const int chunk = max(least, (quotient(held + a.n_split - 1, a.by_split) + kPageRows - 1) / kPageRows * kPageRows);
     const int used = (keys + chunk - 1) / chunk;
@@ -544,6 +544,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
     if (threadIdx.x == 0) __hip_atomic_store(ticket, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     // (eight slices at a time: 32 at once 17.3 us for 8 tokens x 32 / 8 heads x 16000 keys, 14.8 so; several waves a column: even)
     constexpr int kBatch = 8;
+    static_assert(kDecodeMaxSplit <= 64, "a lane weighs a slice");
     for (int q = wave; q < cols; q += WAVES) {
         const float* const p = part0 + q * kPartStride;
         // (the first slices' numerators are requested before their weights are known)

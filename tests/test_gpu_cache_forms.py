@@ -97,3 +97,21 @@ def test_read_past_the_caches(ctx, case, bits):  # noqa: F811
                 there = held[row] - start[row]
                 assert torch.equal(o[row, :, :there], value[w[row, :, start[row]:held[row]]])
                 assert (o[row, :, there:] == 77.0).all()
+
+
+def test_codes_below_bf16_are_cut_off(ctx):  # noqa: F811
+    """fp32 rows near the smallest scale in 8 bits, read back as bf16: the upper halves of what the codes stand for."""
+    print("[case] cache read, smallest codes", flush=True)
+    n, H = 40, 2
+    x = _rows((1, H, n, 128), "f32", 150) * 2.0 ** -130
+    pf, pb = _params("f32", 1, H, H, n), _params("bf16", 1, H, H, n)
+    c = B.QuantCache(pf, n, 8)
+    ctx.tf_cache_write(pf, c.desc, x, x, None, n, None)
+    f, b = (torch.zeros((1, H, n, 128), dtype=DT[dt], device="cuda") for dt in ("f32", "bf16"))
+    ctx.tf_cache_read(pf, c.desc, None, f, f.clone())
+    ctx.tf_cache_read(pb, c.desc, None, b, b.clone())
+    torch.cuda.synchronize()
+    want = torch.from_numpy(ref.values(*ref.quantise(x.double().cpu().numpy(), 8), 8))
+    assert torch.equal(f.cpu().double(), want)
+    assert torch.equal(b.view(torch.int16).int() & 0xFFFF, (f.view(torch.int32) >> 16) & 0xFFFF)
+    assert not torch.equal(b.float(), f)
