@@ -189,10 +189,12 @@ __device__ __forceinline__ void store_pair(float* p, float x, float y) { *reinte
 // (The scaled 4-bit product, which would take codes as they are, adds up with less than fp32: 1.5e-4 of the sum of
 // magnitudes was measured, and queries would have to be rounded to 8 bits.)
 // What bounds it: long caches the way of their bytes (8 x 32 heads x 8192 keys in 4 bits, 285 MB: 51 us, 5.6 TB/s),
-// many queries both pipes (2 x 256 queries x 6000 keys, 40.7 GFLOP: 57 us, 8.9 us for each 1024 keys more, which is
-// 0.95 PFLOP/s where a large library product reaches 1.25; without its exponentials 54.5, without converting codes 53,
-// with all pages from the caches 58), short caches a chain of latencies (32 / 8 heads x 500 keys: 5.9 us, of which a
-// launch with one load takes 2.5).
+// many queries the vector unit and the matrix pipe, mostly in turn: 2 x 256 queries x 6000 keys, 40.7 GFLOP, 59 us, 9.2
+// to 10 us for each 1024 keys more, which is 0.86 to 0.93 PFLOP/s where a large library product reaches 1.25; vector
+// instructions are under way 56 % of the time, matrix ones 30 %, 65 and 35 % in 4 x 512 x 8000 (of 57 us once, without
+// exponentials 54.5, without converting codes 53).  Between them every tile of 16 columns converts a cache's pages again:
+// 64 queries x 8000 keys 24.5 us, 51 and 20 %.  Short caches are a chain of latencies (32 / 8 heads x 500 keys: 5.9 us, of
+// which a launch with one load takes 2.5).
 
 // Parts of two values: three of them cut off, which is exact, or two rounded.
 template <int PARTS>
