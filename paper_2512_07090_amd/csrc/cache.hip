@@ -411,10 +411,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attend_kernel(const Cache
 #pragma unroll
                 for (int i = 0; i < 8; ++i) acc[ct][i] *= down;
             }
-            // Weights are exp2(s scale - mx) in one rounding.  Beyond 2^24 what the maximum lost in its own could overflow an
-            // exponent, so scores are rounded like it there: equal ones have equal weights, whatever their size.
+            // Weights are exp2(s scale - mx) in one rounding, in which what the maximum lost in its own is a factor that cancels.
+            // Beyond 2^28 that could be more than 2^16, and overflow further on: scores are rounded like the maximum there, so
+            // that equal ones have equal weights, whatever their size.
             factor[ct] = a.scale_log2e;
-            const bool far = fabsf(mx[ct]) > 0x1p24f && mx[ct] > kNoKey;
+            const bool far = fabsf(mx[ct]) > 0x1p28f && mx[ct] > kNoKey;
             if (__any(far)) {
                 const float first = far ? a.scale_log2e : 1.f;   // (a column's own: its neighbours keep their rounding)
                 factor[ct] = far ? 1.f : a.scale_log2e;
